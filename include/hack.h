@@ -284,6 +284,78 @@ HACK_API int32_t hack_debug_build(void);
  * that no longer hold their pattern; hack_last_error() names the first.  UNSUPPORTED in the normal
  * build. */
 HACK_API hack_status_t hack_debug_check(hack_cache_t* cache, int32_t* violations);
+/* ------------------------------------------------------------------------------------------------
+ * From a layer's projections to its steps: rotary positions and norms of queries and keys.
+ *
+ * A tensor here is [batch, heads, tokens, head_dim] with any strides but the last, which is 1: a view
+ * of the projection's output [batch, tokens, heads, head_dim] as well as the dense layout of the steps.
+ * Every row starts on a 16-byte boundary (base address and strides).  head_dim is 64 or 128, dtype
+ * HACK_F32 or HACK_BF16; sums and products are fp32, rounded once.  Nothing is allocated or kept.
+ * An output may be its input (same address, same strides); other overlaps are not allowed.
+ * A call with no tokens does nothing.  `device` is made current for the call.
+ * ---------------------------------------------------------------------------------------------- */
+typedef struct { int64_t batch, head, token; } hack_strides_t;   /* in elements */
+
+enum { HACK_ROPE_HALF = 0,    /* element i of the rotated part pairs with element i + rotary_dim / 2 */
+       HACK_ROPE_PAIRS = 1 }; /* element 2i pairs with element 2i + 1 */
+/* Frequencies of contexts longer than the trained one (D: dimensions an axis rotates, factor: the stretch) */
+enum { HACK_ROPE_PLAIN = 0,   /* f_i = base^(-2i / D) */
+       HACK_ROPE_LINEAR = 1,  /* f_i / factor */
+       HACK_ROPE_BASE = 2,    /* base grows to base * factor^(D / (D - 2)) */
+       HACK_ROPE_BANDS = 3 }; /* pairs that turn more than turns_fast times within trained_length stay as they are, those
+                                 that turn less than turns_slow times are divided by factor, a linear ramp over the pair
+                                 numbers between; cosine and sine are multiplied by 1 + 0.1 ln(factor) */
+#define HACK_ROPE_MAX_PAIRS 64
+
+/* A rotation.  Plain data, filled by hack_rope_plan (or by the caller); nothing on a device belongs to it.
+ * Pair i of a token at position p turns by the angle p * freq[i], formed in 64 bits:
+ *   y0 = gain * (x0 cos - x1 sin),  y1 = gain * (x0 sin + x1 cos).
+ * With two axes a token has two positions (a grid's row and column): the first half of the pairs turns by the
+ * first, the second half by the second.  Elements from rotary_dim on pass unchanged. */
+typedef struct {
+  int32_t head_dim, rotary_dim, layout, axes;
+  float gain;
+  int32_t reserved;
+  double freq[HACK_ROPE_MAX_PAIRS];
+} hack_rope_plan_t;
+
+/* Host only.  rotary_dim: a multiple of 2 * axes in 2..head_dim.  turns_fast, turns_slow: 0 selects 32 and 1. */
+HACK_API hack_status_t hack_rope_plan(int32_t head_dim, int32_t rotary_dim, int32_t layout, int32_t axes, double base,
+                                      int32_t scaling, double factor, int64_t trained_length, double turns_fast,
+                                      double turns_slow, hack_rope_plan_t* out);
+
+typedef struct {
+  int32_t device, dtype, batch, n_heads, n_tokens;
+  int32_t transpose;          /* 1: by the opposite angles, which is the gradient of the rotation */
+  int32_t positions_f32;      /* positions: 0 int32, 1 fp32; [batch, n_tokens, axes] */
+  int32_t reserved;
+  int64_t positions_stride;   /* elements from one batch element's positions to the next's; 0: shared */
+  hack_strides_t x, y;
+} hack_rope_args_t;
+/* y = x with the rotation of its token's position. */
+HACK_API hack_status_t hack_rope(const hack_rope_plan_t* plan, const hack_rope_args_t* args, const void* x, void* y,
+                                 const void* positions, void* stream);
+
+enum { HACK_NORM_NONE = 0,
+       HACK_NORM_RMS = 1,     /* x / sqrt(mean x^2 + eps) */
+       HACK_NORM_L2 = 2 };    /* x / max(|x|, eps) */
+typedef struct {
+  int32_t device, dtype, batch, n_heads, n_kv_heads, n_tokens, head_dim;
+  int32_t norm;               /* HACK_NORM_*, of every row of q and k on its own */
+  float eps;
+  int32_t positions_f32;
+  int64_t positions_stride;
+  hack_strides_t q, k, v, q_out, k_out, v_out;
+} hack_qkv_args_t;
+/* Queries and keys normalised per head, multiplied by a weight per channel (fp32 [head_dim], may be NULL) and a gain
+ * per head (fp32 [n_heads] or [n_kv_heads], may be NULL), and rotated (plan and positions NULL: not); values
+ * copied: one pass from the projection's output to what hack_scale_step takes.  v and v_out may both be NULL, and so
+ * may k and k_out. */
+HACK_API hack_status_t hack_qk_norm_rope(const hack_rope_plan_t* plan, const hack_qkv_args_t* args, const void* q, const void* k,
+                                         const void* v, void* q_out, void* k_out, void* v_out, const void* positions,
+                                         const float* q_weight, const float* k_weight, const float* q_gain,
+                                         const float* k_gain, void* stream);
+
 /* Text of the calling thread's last error; never NULL. */
 HACK_API const char* hack_last_error(void);
 

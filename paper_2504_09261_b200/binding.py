@@ -24,6 +24,9 @@ HACK_F32, HACK_BF16 = 0, 1
 HACK_OVERFLOW_KEEP_PROTECTED, HACK_OVERFLOW_COMPETE = 0, 1
 HACK_OBS_UNIFORM, HACK_OBS_INIT, HACK_OBS_RECENT, HACK_OBS_CALLER, HACK_OBS_FULL = 0, 1, 2, 3, 4
 RULE_FRACTION, RULE_RATIO = 0, 1
+HACK_ROPE_HALF, HACK_ROPE_PAIRS = 0, 1
+HACK_ROPE_PLAIN, HACK_ROPE_LINEAR, HACK_ROPE_BASE, HACK_ROPE_BANDS = 0, 1, 2, 3
+HACK_NORM_NONE, HACK_NORM_RMS, HACK_NORM_L2 = 0, 1, 2
 
 EXPORTS = (
     "hack_split_budget", "hack_init_cache", "hack_free_cache", "hack_reset", "hack_set_obs_rows", "hack_get_limits",
@@ -32,6 +35,7 @@ EXPORTS = (
     "hack_scale_step_host", "hack_score_noalloc", "hack_get_lengths", "hack_read_head", "hack_kv_bytes",
     "hack_launch_count", "hack_stage_timing", "hack_stage_times", "hack_poll_status", "hack_set_wait_limit",
     "hack_debug_build", "hack_debug_check", "hack_last_error",
+    "hack_rope_plan", "hack_rope", "hack_qk_norm_rope",
 )
 
 
@@ -54,6 +58,29 @@ class HackStepInfo(C.Structure):
 
 class HackLimits(C.Structure):
     _fields_ = [("cand_stride", C.c_int32), ("kept_stride", C.c_int32), ("max_new", C.c_int32)]
+
+
+class HackStrides(C.Structure):
+    _fields_ = [("batch", C.c_int64), ("head", C.c_int64), ("token", C.c_int64)]
+
+
+class HackRopePlan(C.Structure):
+    """A rotation: plain data, which hack_rope_plan fills."""
+    _fields_ = [("head_dim", C.c_int32), ("rotary_dim", C.c_int32), ("layout", C.c_int32), ("axes", C.c_int32),
+                ("gain", C.c_float), ("reserved", C.c_int32), ("freq", C.c_double * 64)]
+
+
+class HackRopeArgs(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("device", "dtype", "batch", "n_heads", "n_tokens", "transpose", "positions_f32",
+                                         "reserved")] + [
+        ("positions_stride", C.c_int64), ("x", HackStrides), ("y", HackStrides)]
+
+
+class HackQkvArgs(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("device", "dtype", "batch", "n_heads", "n_kv_heads", "n_tokens", "head_dim",
+                                         "norm")] + [
+        ("eps", C.c_float), ("positions_f32", C.c_int32), ("positions_stride", C.c_int64)] + [
+        (n, HackStrides) for n in ("q", "k", "v", "q_out", "k_out", "v_out")]
 
 
 class HackError(RuntimeError):
@@ -98,6 +125,9 @@ def _load() -> C.CDLL:
         "hack_stage_timing": [vp, i32],
         "hack_stage_times": [vp, C.POINTER(C.c_double), C.POINTER(C.c_uint64)],
     }
+    sigs["hack_rope_plan"] = [i32, i32, i32, i32, C.c_double, i32, C.c_double, C.c_int64, C.c_double, C.c_double, vp]
+    sigs["hack_rope"] = [vp] * 6
+    sigs["hack_qk_norm_rope"] = [vp] * 14
     for name, args in sigs.items():
         fn = getattr(lib, name)
         fn.argtypes = args
@@ -111,25 +141,34 @@ lib = _load()
 
 
 def _load_call():
-    """call(address, handle, layer, scale, *buffers) -> status: the compiled marshalling of the per-step
-    entry points, or the same through ctypes if the module was not built for this interpreter."""
+    """call(address, handle, layer, scale, *buffers) -> status, invoke(address, *buffers) -> status and key(*tensors): the
+    compiled marshalling of the entry points that run step by step, or the same through ctypes if the module was not built for
+    this interpreter."""
     path = os.path.join(os.path.dirname(_LIB_PATH), "_hackcall" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
     if os.path.exists(path):
         spec = importlib.util.spec_from_file_location("_hackcall", path)
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
-        return module.call
-    functions = {C.cast(getattr(lib, n), C.c_void_p).value: getattr(lib, n)
+        if hasattr(module, "invoke"):
+            return module.call, module.invoke, module.key
+    functions = {_address(n): getattr(lib, n)
                  for n in ("hack_score", "hack_select", "hack_compact", "hack_attend", "hack_attend_variance",
-                           "hack_scale_step", "hack_scale_step_host")}
-    return lambda address, handle, layer, scale, *buffers: functions[address](handle, layer, scale, *map(_ptr, buffers))
+                           "hack_scale_step", "hack_scale_step_host") + _INVOKED}
+    return (lambda address, handle, layer, scale, *buffers: functions[address](handle, layer, scale, *map(_ptr, buffers)),
+            lambda address, *buffers: functions[address](*map(_ptr, buffers)),
+            lambda *tensors: tuple(None if x is None else (x.dtype, x.shape, x.stride(), x.get_device()) for x in tensors))
 
 
-_call = _load_call()
-_SCORE, _SELECT, _COMPACT, _ATTEND, _ATTEND_VARIANCE, _SCALE_STEP, _SCALE_STEP_HOST = (
-    C.cast(getattr(lib, n), C.c_void_p).value for n in (
-        "hack_score", "hack_select", "hack_compact", "hack_attend", "hack_attend_variance", "hack_scale_step",
-        "hack_scale_step_host"))
+def _address(name: str) -> int:
+    return C.cast(getattr(lib, name), C.c_void_p).value
+
+
+_INVOKED = ("hack_rope", "hack_qk_norm_rope")
+_call, _invoke, _key = _load_call()
+_SCORE, _SELECT, _COMPACT, _ATTEND, _ATTEND_VARIANCE, _SCALE_STEP, _SCALE_STEP_HOST = map(_address, (
+    "hack_score", "hack_select", "hack_compact", "hack_attend", "hack_attend_variance", "hack_scale_step",
+    "hack_scale_step_host"))
+_ROPE, _QK_NORM_ROPE = map(_address, _INVOKED)
 
 
 def hack_last_error() -> str:
@@ -163,6 +202,132 @@ def hack_score_noalloc(q, k_cand, scores, n_rows: int, n_queries: int, n_cand: i
     """Scores on dense device tensors with no device allocation (fixed in-library scratch)."""
     _check(lib.hack_score_noalloc(_ptr(q), _ptr(k_cand), _ptr(scores), n_rows, n_queries, n_cand,
                                   score_stride, head_dim, dtype, n_obs, sm_scale, _ptr(stream)))
+
+
+# ------------------------------------------------------------------ tensors [batch, heads, tokens, head_dim]
+_DTYPES = {}
+
+
+def _dtype_of(x) -> int:
+    """HACK_F32 or HACK_BF16 of a tensor."""
+    d = _DTYPES.get(x.dtype)
+    if d is None:
+        d = {"torch.float32": HACK_F32, "torch.bfloat16": HACK_BF16}.get(str(x.dtype))
+        if d is None:
+            raise ValueError(f"dtype {x.dtype}: float32 and bfloat16 are served")
+        _DTYPES[x.dtype] = d
+    return d
+
+
+def _strides_of(x, what: str) -> HackStrides:
+    s = x.stride()
+    if len(s) != 4 or (s[3] != 1 and x.shape[3] != 1):
+        raise ValueError(f"{what} must be [batch, heads, tokens, head_dim] with contiguous rows")
+    return HackStrides(s[0], s[1], s[2])
+
+
+def _same(what: str, *tensors) -> None:
+    """Same dtype, same device."""
+    first = tensors[0]
+    for t in tensors[1:]:
+        if t is not None and (t.dtype != first.dtype or t.get_device() != first.get_device()):
+            raise ValueError(f"{what}: tensors of different types or devices")
+
+
+def _positions(positions, batch: int, n_tokens: int, axes: int, device: int):
+    """(positions_f32, positions_stride) of [tokens(, axes)] or [batch, tokens(, axes)]."""
+    f32 = {"torch.int32": 0, "torch.float32": 1}.get(str(positions.dtype))
+    if f32 is None:
+        raise ValueError("positions must be int32 or float32")
+    if positions.get_device() != device or not positions.is_contiguous():
+        raise ValueError("positions must be contiguous and on the tensors' device")
+    shape, own = tuple(positions.shape), (n_tokens,) if axes == 1 else (n_tokens, axes)
+    if shape == own:
+        return f32, 0
+    if shape == (batch,) + own:
+        return f32, n_tokens * axes
+    raise ValueError(f"positions of shape {shape}: [batch,] {own} wanted")
+
+
+def _float_vector(x, n: int, device: int, what: str) -> None:
+    if x is not None and (str(x.dtype) != "torch.float32" or x.numel() != n or not x.is_contiguous() or x.get_device() != device):
+        raise ValueError(f"{what} must be {n} contiguous float32 values on the tensors' device")
+
+
+_args_of = {}     # argument structs by shapes, strides and types: they hold nothing of a call's tensors
+
+
+def _cached(key, make):
+    args = _args_of.get(key)
+    if args is None:
+        if len(_args_of) >= 4096:
+            _args_of.clear()
+        made = make()
+        args = _args_of[key] = (made, C.addressof(made))
+    return args[1]
+
+
+def hack_rope_plan(head_dim: int, rotary_dim: Optional[int] = None, layout: int = HACK_ROPE_HALF, axes: int = 1,
+                   base: float = 10000.0, scaling: int = HACK_ROPE_PLAIN, factor: float = 1.0, trained_length: int = 0,
+                   turns_fast: float = 0.0, turns_slow: float = 0.0) -> HackRopePlan:
+    plan = HackRopePlan()
+    _check(lib.hack_rope_plan(head_dim, head_dim if rotary_dim is None else rotary_dim, layout, axes, base, scaling, factor,
+                              trained_length, turns_fast, turns_slow, C.byref(plan)))
+    return plan
+
+
+def hack_rope(plan: HackRopePlan, x, y, positions, transpose: bool = False, stream=None) -> None:
+    """y = x rotated to its tokens' positions.  x, y: [batch, heads, tokens, head_dim], any strides but the last; positions:
+    int32 or float32 [batch,] tokens[, axes]."""
+    axes = plan.axes
+
+    def make():
+        _same("hack_rope", x, y)
+        b, h, n, d = x.shape
+        if tuple(y.shape) != (b, h, n, d) or d != plan.head_dim:
+            raise ValueError("x and y must have the same shape, with the plan's head_dim")
+        f32, stride = _positions(positions, b, n, axes, x.get_device())
+        return HackRopeArgs(x.get_device(), _dtype_of(x), b, h, n, int(transpose), f32, 0, stride, _strides_of(x, "x"),
+                            _strides_of(y, "y"))
+
+    args = _cached((axes, plan.head_dim, transpose, _key(x, y, positions)), make)
+    status = _invoke(_ROPE, C.addressof(plan), args, x, y, positions, stream)
+    if status:
+        _check(status)
+
+
+def _qkv_args(plan, q, k, v, q_out, k_out, v_out, positions, norm, eps, q_weight, k_weight, q_gain, k_gain):
+    _same("hack_qk_norm_rope", q, k, v, q_out, k_out, v_out)
+    b, h, n, d = q.shape
+    kv = k if k is not None else v
+    kv_heads = kv.shape[1] if kv is not None else 0
+    for t, o, heads, what in ((q, q_out, h, "q"), (k, k_out, kv_heads, "k"), (v, v_out, kv_heads, "v")):
+        if (t is None) != (o is None):
+            raise ValueError(f"{what} and its output: both or neither")
+        if t is not None and (tuple(t.shape) != (b, heads, n, d) or t.shape != o.shape):
+            raise ValueError(f"{what}: shapes differ")
+    dev = q.get_device()
+    _float_vector(q_weight, d, dev, "q_weight")
+    _float_vector(k_weight, d, dev, "k_weight")
+    _float_vector(q_gain, h, dev, "q_gain")
+    _float_vector(k_gain, kv_heads, dev, "k_gain")
+    f32, stride = _positions(positions, b, n, plan.axes, dev) if positions is not None and plan is not None else (0, 0)
+    none = HackStrides()
+    return HackQkvArgs(dev, _dtype_of(q), b, h, kv_heads, n, d, norm, eps, f32, stride,
+                       *(none if t is None else _strides_of(t, "a tensor") for t in (q, k, v, q_out, k_out, v_out)))
+
+
+def hack_qk_norm_rope(plan: Optional[HackRopePlan], q, k, v, q_out, k_out, v_out, positions, norm: int = HACK_NORM_RMS,
+                      eps: float = 1e-6, q_weight=None, k_weight=None, q_gain=None, k_gain=None, stream=None) -> None:
+    """Queries and keys normalised per head, weighted and rotated, values copied: from views of a projection's output to the
+    layout of the steps.  All tensors [batch, heads, tokens, head_dim]; plan and positions None: no rotation."""
+    args = _cached((None if plan is None else (plan.axes, plan.head_dim), norm, eps,
+                    _key(q, k, v, q_out, k_out, v_out, positions, q_weight, k_weight, q_gain, k_gain)),
+                   lambda: _qkv_args(plan, q, k, v, q_out, k_out, v_out, positions, norm, eps, q_weight, k_weight, q_gain, k_gain))
+    status = _invoke(_QK_NORM_ROPE, None if plan is None else C.addressof(plan), args, q, k, v, q_out, k_out, v_out, positions,
+                     q_weight, k_weight, q_gain, k_gain, stream)
+    if status:
+        _check(status)
 
 
 def _ptr(x) -> Optional[int]:

@@ -9,6 +9,7 @@
 #include <new>
 #include <utility>
 
+#include "device_scope.h"
 #include "hack_internal.h"
 
 namespace hack {
@@ -261,26 +262,7 @@ hack::StepArgs make_args(const hack_cache* c, int layer, int scale, const hack_s
 
 size_t live_bytes(const hack_cache* c) { return (size_t)c->live_rows * c->cfg.head_dim * c->elt * 2; }
 
-// Makes the cache's device current for the duration of an entry point and puts the caller's back.
-struct DeviceScope {
-  int prev = -1;
-  bool switched = false;
-  cudaError_t err = cudaSuccess;
-  explicit DeviceScope(int want) {
-    err = cudaGetDevice(&prev);
-    if (err == cudaSuccess && prev != want) {
-      err = cudaSetDevice(want);
-      switched = err == cudaSuccess;
-    }
-  }
-  ~DeviceScope() { if (switched) cudaSetDevice(prev); }
-};
-#define HACK_ON_DEVICE(c)                                                                        \
-  DeviceScope dev_scope_((c)->cfg.device);                                                       \
-  if (dev_scope_.err != cudaSuccess) {                                                           \
-    set_error(std::string("selecting the cache's device: ") + cudaGetErrorString(dev_scope_.err)); \
-    return HACK_ERR_CUDA;                                                                        \
-  }
+#define HACK_ON_DEVICE(c) HACK_ON_DEVICE_OF((c)->cfg.device)
 
 // A launcher failed after earlier launches of the same step were enqueued: the device-side state
 // of the layer no longer matches the host's plan, so the cache refuses further steps until reset.

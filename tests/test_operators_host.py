@@ -1,0 +1,83 @@
+"""Refusals of the operators around the cache: on the host, before anything is launched (no GPU needed)."""
+import ctypes as C
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def hb():
+    import __graft_entry__ as ge
+    ge.build()
+    import paper_2504_09261_b200 as pkg
+    return pkg
+
+
+GOOD = dict(head_dim=128, rotary_dim=64, layout=0, axes=1, base=10000.0, scaling=0, factor=1.0, trained_length=0)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(head_dim=96), 2), (dict(rotary_dim=0), 1), (dict(rotary_dim=130), 1), (dict(rotary_dim=63), 1), (dict(rotary_dim=62, axes=2), 1),
+    (dict(axes=3), 1), (dict(layout=2), 1), (dict(base=1.0), 1), (dict(base=float("nan")), 1), (dict(scaling=4), 1),
+    (dict(scaling=1, factor=0.5), 1), (dict(scaling=2, factor=float("inf")), 1), (dict(scaling=3, factor=2.0), 1),
+    (dict(scaling=3, factor=2.0, trained_length=4096, turns_fast=1.0, turns_slow=2.0), 1)])
+def test_rope_plan_refuses(hb, change, status):
+    hb.hack_rope_plan(**GOOD)
+    with pytest.raises(hb.HackError) as e:
+        hb.hack_rope_plan(**{**GOOD, **change})
+    assert e.value.status == status and str(e.value)
+
+
+def _rope_args(**change):
+    from paper_2504_09261_b200 import binding as bd
+    a = dict(device=0, dtype=1, batch=2, n_heads=3, n_tokens=4, positions_stride=0)
+    a.update({k: v for k, v in change.items() if k in a})
+    args = bd.HackRopeArgs(**a)
+    args.x = args.y = bd.HackStrides(3 * 4 * 128, 4 * 128, 128)
+    for k, v in change.items():
+        if k in ("x", "y"):
+            setattr(args, k, bd.HackStrides(*v))
+    return args
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(dtype=2), 2), (dict(batch=0), 1), (dict(n_heads=0), 1), (dict(n_tokens=-1), 1), (dict(device=-1), 1),
+    (dict(x=(1536, 512, 124)), 1), (dict(y=(1536, 512, 64)), 1), (dict(y=(0, 512, 128)), 1), (dict(y=(1536, 256, 128)), 1),
+    (dict(y=(-1536, 512, 128)), 1)])
+def test_rope_refuses(hb, change, status):
+    from paper_2504_09261_b200 import binding as bd
+    plan = hb.hack_rope_plan(128)
+    args = _rope_args(**change)
+    assert bd.lib.hack_rope(C.addressof(plan), C.addressof(args), 4096, 8192, 16384, None) == status
+    assert hb.hack_last_error()
+
+
+def test_rope_refuses_pointers(hb):
+    from paper_2504_09261_b200 import binding as bd
+    plan, args = hb.hack_rope_plan(128), _rope_args()
+    p, a = C.addressof(plan), C.addressof(args)
+    for call in ((None, a, 4096, 8192, 16384), (p, None, 4096, 8192, 16384), (p, a, None, 8192, 16384), (p, a, 4096, None, 16384),
+                 (p, a, 4096, 8192, None), (p, a, 4104, 8192, 16384), (p, a, 4096, 8194, 16384)):
+        assert bd.lib.hack_rope(*call, None) == 1, call
+    blank = bd.HackRopePlan()
+    blank.head_dim = 128
+    assert bd.lib.hack_rope(C.addressof(blank), a, 4096, 8192, 16384, None) == 1
+    nothing = _rope_args(n_tokens=0)
+    assert bd.lib.hack_rope(p, C.addressof(nothing), None, None, None, None) == 0
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(dtype=7), 2), (dict(head_dim=80), 2), (dict(norm=3), 1), (dict(eps=0.0), 1), (dict(eps=float("nan")), 1), (dict(n_kv_heads=0), 1),
+    (dict(v_out=None), 1), (dict(k=None), 1), (dict(positions=None), 1), (dict(plan=None), 1), (dict(q=None), 1), (dict(plan="other"), 1)])
+def test_qk_norm_rope_refuses(hb, change, status):
+    from paper_2504_09261_b200 import binding as bd
+    plan = hb.hack_rope_plan(64 if change.get("plan") == "other" else 128)
+    f = dict(device=0, dtype=0, batch=1, n_heads=2, n_kv_heads=2, n_tokens=3, head_dim=128, norm=1, eps=1e-6)
+    f.update({k: v for k, v in change.items() if k in f})
+    args = bd.HackQkvArgs(**f)
+    for name in ("q", "k", "v", "q_out", "k_out", "v_out"):
+        setattr(args, name, bd.HackStrides(768, 384, 128))
+    ptr = dict(q=4096, k=8192, v=12288, q_out=16384, k_out=20480, v_out=24576, positions=28672)
+    ptr.update({k: v for k, v in change.items() if k in ptr})
+    p = None if "plan" in change and change["plan"] is None else C.addressof(plan)
+    assert bd.lib.hack_qk_norm_rope(p, C.addressof(args), *ptr.values(), None, None, None, None, None) == status
+    assert hb.hack_last_error()
