@@ -356,6 +356,80 @@ HACK_API hack_status_t hack_qk_norm_rope(const hack_rope_plan_t* plan, const hac
                                          const float* q_weight, const float* k_weight, const float* q_gain,
                                          const float* k_gain, void* stream);
 
+/* hack_scale_step from the projections of a layer: hack_qk_norm_rope into buffers of the cache's own (created by the first
+ * call on a cache, which must be outside any stream capture), then the step.  args describe the inputs, with as many
+ * key as query heads, n_tokens = N_k of the scale and the cache's batch, heads, head_dim, dtype and device; its output strides are
+ * not looked at.  out: dense [batch, n_heads, N_k, head_dim]. */
+HACK_API hack_status_t hack_scale_step_qkv(hack_cache_t* cache, int32_t layer, int32_t scale, const hack_rope_plan_t* plan,
+                                           const hack_qkv_args_t* args, const void* q, const void* k, const void* v,
+                                           const void* positions, const float* q_weight, const float* k_weight,
+                                           const float* q_gain, const float* k_gain, void* out, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Caches of 4 bits: rows of keys and values in a little over a quarter of their bf16 bytes, and the
+ * attention that reads them.
+ *
+ * A row of head_dim elements is blocks of 16 that share a scale s, one of the 256 values
+ * (1 + m/8) 2^(e-20), byte 8 e + m: the smallest with 7 s >= the block's largest |x|, or the largest
+ * of all.  An element is c * s, c = x / s rounded to the nearest whole number (ties to even) and
+ * limited to -7..7; byte j of a row holds c + 8 of element 2j in its low and of element 2j + 1 in its
+ * high half.  c * s has no more than seven significant bits: bf16 holds it exactly.  NaN is stored as
+ * 0, what is beyond 26 880 as that.
+ * The planes are the caller's device buffers, 16-byte aligned: codes [rows, head_dim / 2] and scales
+ * [rows, head_dim / 16] bytes of K and of V.  Head i = b * n_kv_heads + h owns rows
+ * [first, first + cap), first = row_off[i] (device) or, row_off NULL, i * cap.  How many of them are
+ * in use is the caller's to keep, on the device, so that a captured graph can be replayed with other
+ * lengths: lens, int32 [batch * n_kv_heads].  The library only reads it; a length below 0 counts as
+ * 0, one beyond cap as cap.
+ * new_lens (device, int32 [batch], may be NULL): of a padded batch, how many of the call's tokens each
+ * batch element really has; the others are not read, and their outputs are left as they were.
+ * ---------------------------------------------------------------------------------------------- */
+typedef struct {
+  int32_t device, batch, n_kv_heads, head_dim;   /* head_dim 64 or 128 */
+  int32_t cap, reserved;
+  const int64_t* row_off;
+  void *k_codes, *v_codes, *k_scales, *v_scales;
+} hack_kv4_t;
+
+typedef struct {
+  int32_t dtype, n_tokens;
+  hack_strides_t k, v;
+} hack_kv4_rows_t;
+/* Rows k, v [batch, n_kv_heads, n_tokens, head_dim] join behind the lens rows of every head; rows that would
+ * not fit are dropped.  The step after it is hack_kv4_attend with `appended`, and then lens += n_tokens, by
+ * the caller. */
+HACK_API hack_status_t hack_kv4_append(const hack_kv4_t* kv, const hack_kv4_rows_t* rows, const void* k, const void* v,
+                                       const int32_t* lens, const int32_t* new_lens, void* stream);
+/* The values of rows first[i] .. first[i] + n_tokens - 1 of every head, in dense or strided tensors (k, v of
+ * `rows` are the outputs' strides); rows outside [0, cap) give zeros. */
+HACK_API hack_status_t hack_kv4_read(const hack_kv4_t* kv, const hack_kv4_rows_t* rows, void* k_out, void* v_out,
+                                     const int32_t* first, void* stream);
+/* The rows that a layer of a cache holds (every head its own number of them, hack_get_lengths) join a 4-bit
+ * cache of the same batch, heads and head_dim behind its lens rows. */
+HACK_API hack_status_t hack_store_kv4(hack_cache_t* cache, int32_t layer, const hack_kv4_t* kv, const int32_t* lens,
+                                      void* stream);
+
+typedef struct {
+  int32_t dtype;                 /* of q and out */
+  int32_t n_heads, n_queries;    /* n_heads a multiple of n_kv_heads: query head h reads stored head h / (n_heads / n_kv_heads) */
+  int32_t max_len;               /* no head attends over more rows (launches are planned for it); rows behind it are not seen */
+  int32_t appended;              /* 1: the n_queries (or new_lens[b]) rows behind lens count too: those just appended */
+  int32_t causal;                /* 1: query i of n, at position length - n + i, sees no later rows */
+  int32_t window, n_sink;        /* window > 0: of the rows up to its position a query sees the last `window` (itself
+                                    counted) and the first n_sink */
+  float sm_scale;                /* 0 selects 1 / sqrt(head_dim) */
+  int32_t reserved;
+  int64_t workspace_bytes;       /* size of the workspace given */
+  hack_strides_t q, out;
+} hack_kv4_attend_t;
+/* Device memory that a call of these sizes needs (it may be 0); it depends on the struct's sizes alone. */
+HACK_API hack_status_t hack_kv4_workspace(const hack_kv4_t* kv, const hack_kv4_attend_t* args, size_t* bytes);
+/* O = Softmax(sm_scale Q K^T) V over the stored rows that a query sees; a query that sees none gets zeros.  Logits,
+ * softmax and sums in fp32.  workspace: 16-byte aligned, its contents need no preparation and mean nothing after the call;
+ * calls that may overlap on the GPU need workspaces of their own. */
+HACK_API hack_status_t hack_kv4_attend(const hack_kv4_t* kv, const hack_kv4_attend_t* args, const void* q, void* out,
+                                       const int32_t* lens, const int32_t* new_lens, void* workspace, void* stream);
+
 /* Text of the calling thread's last error; never NULL. */
 HACK_API const char* hack_last_error(void);
 

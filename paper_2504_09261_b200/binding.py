@@ -35,7 +35,8 @@ EXPORTS = (
     "hack_scale_step_host", "hack_score_noalloc", "hack_get_lengths", "hack_read_head", "hack_kv_bytes",
     "hack_launch_count", "hack_stage_timing", "hack_stage_times", "hack_poll_status", "hack_set_wait_limit",
     "hack_debug_build", "hack_debug_check", "hack_last_error",
-    "hack_rope_plan", "hack_rope", "hack_qk_norm_rope",
+    "hack_rope_plan", "hack_rope", "hack_qk_norm_rope", "hack_scale_step_qkv", "hack_kv4_append", "hack_kv4_read",
+    "hack_store_kv4", "hack_kv4_workspace", "hack_kv4_attend",
 )
 
 
@@ -83,6 +84,20 @@ class HackQkvArgs(C.Structure):
         (n, HackStrides) for n in ("q", "k", "v", "q_out", "k_out", "v_out")]
 
 
+class HackKv4Planes(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("device", "batch", "n_kv_heads", "head_dim", "cap", "reserved")] + [
+        (n, C.c_void_p) for n in ("row_off", "k_codes", "v_codes", "k_scales", "v_scales")]
+
+
+class HackKv4Rows(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_tokens", C.c_int32), ("k", HackStrides), ("v", HackStrides)]
+
+
+class HackKv4Attend(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_heads", "n_queries", "max_len", "appended", "causal", "window", "n_sink")] + [
+        ("sm_scale", C.c_float), ("reserved", C.c_int32), ("workspace_bytes", C.c_int64), ("q", HackStrides), ("out", HackStrides)]
+
+
 class HackError(RuntimeError):
     def __init__(self, status: int, text: str):
         super().__init__(f"hack status {status}: {text}")
@@ -128,6 +143,12 @@ def _load() -> C.CDLL:
     sigs["hack_rope_plan"] = [i32, i32, i32, i32, C.c_double, i32, C.c_double, C.c_int64, C.c_double, C.c_double, vp]
     sigs["hack_rope"] = [vp] * 6
     sigs["hack_qk_norm_rope"] = [vp] * 14
+    sigs["hack_scale_step_qkv"] = [vp, i32, i32] + [vp] * 12
+    sigs["hack_kv4_append"] = [vp] * 7
+    sigs["hack_kv4_read"] = [vp] * 6
+    sigs["hack_store_kv4"] = [vp, i32, vp, vp, vp]
+    sigs["hack_kv4_workspace"] = [vp, vp, C.POINTER(C.c_size_t)]
+    sigs["hack_kv4_attend"] = [vp] * 8
     for name, args in sigs.items():
         fn = getattr(lib, name)
         fn.argtypes = args
@@ -163,12 +184,12 @@ def _address(name: str) -> int:
     return C.cast(getattr(lib, name), C.c_void_p).value
 
 
-_INVOKED = ("hack_rope", "hack_qk_norm_rope")
+_INVOKED = ("hack_rope", "hack_qk_norm_rope", "hack_kv4_append", "hack_kv4_read", "hack_kv4_attend")
 _call, _invoke, _key = _load_call()
 _SCORE, _SELECT, _COMPACT, _ATTEND, _ATTEND_VARIANCE, _SCALE_STEP, _SCALE_STEP_HOST = map(_address, (
     "hack_score", "hack_select", "hack_compact", "hack_attend", "hack_attend_variance", "hack_scale_step",
     "hack_scale_step_host"))
-_ROPE, _QK_NORM_ROPE = map(_address, _INVOKED)
+_ROPE, _QK_NORM_ROPE, _KV4_APPEND, _KV4_READ, _KV4_ATTEND = map(_address, _INVOKED)
 
 
 def hack_last_error() -> str:
@@ -339,6 +360,87 @@ def _ptr(x) -> Optional[int]:
     return x.data_ptr()
 
 
+class HackKv4:
+    """A 4-bit cache on the caller's planes: uint8 tensors [rows, head_dim / 2] (codes) and [rows, head_dim / 16] (scales) of K
+    and V.  Head i = b * n_kv_heads + h owns cap rows, from row i * cap on, or from row_off[i] (int64, on the device).
+    `lens` of the methods: int32 [batch * n_kv_heads] on the device, the rows in use, which is the caller's to keep."""
+
+    def __init__(self, k_codes, k_scales, v_codes, v_scales, batch: int, n_kv_heads: int, cap: int, row_off=None):
+        dim = 2 * k_codes.shape[-1]
+        rows = k_codes.shape[0]
+        for t, width in ((k_codes, dim // 2), (v_codes, dim // 2), (k_scales, dim // 16), (v_scales, dim // 16)):
+            if str(t.dtype) != "torch.uint8" or tuple(t.shape) != (rows, width) or not t.is_contiguous() or \
+                    t.get_device() != k_codes.get_device():
+                raise ValueError("planes must be contiguous uint8 [rows, head_dim / 2] and [rows, head_dim / 16] on one device")
+        if row_off is None:
+            if batch * n_kv_heads * cap > rows:
+                raise ValueError("the planes have fewer than batch * n_kv_heads * cap rows")
+        elif str(row_off.dtype) != "torch.int64" or row_off.numel() != batch * n_kv_heads or not row_off.is_contiguous() or \
+                row_off.get_device() != k_codes.get_device():
+            raise ValueError("row_off must be batch * n_kv_heads contiguous int64 values on the planes' device")
+        self.batch, self.n_kv_heads, self.cap, self.head_dim, self.device = batch, n_kv_heads, cap, dim, k_codes.get_device()
+        self._held = (k_codes, k_scales, v_codes, v_scales, row_off)
+        self._planes = HackKv4Planes(self.device, batch, n_kv_heads, dim, cap, 0, _ptr(row_off), _ptr(k_codes), _ptr(v_codes),
+                                     _ptr(k_scales), _ptr(v_scales))
+        self._address = C.addressof(self._planes)
+
+    def _key(self, *more):
+        return (self.device, self.batch, self.n_kv_heads, self.head_dim) + more
+
+    def _lengths(self, x, n: int, what: str) -> None:
+        if x is not None and (str(x.dtype) != "torch.int32" or x.numel() != n or not x.is_contiguous() or x.get_device() != self.device):
+            raise ValueError(f"{what} must be {n} contiguous int32 values on the cache's device")
+
+    def _rows(self, k, v, lens, new_lens):
+        self._lengths(lens, self.batch * self.n_kv_heads, "lens")
+        self._lengths(new_lens, self.batch, "new_lens")
+        _same("4-bit cache", k, v)
+        if tuple(k.shape) != tuple(v.shape) or len(k.shape) != 4 or tuple(k.shape[:2]) != (self.batch, self.n_kv_heads) or \
+                k.shape[3] != self.head_dim or k.get_device() != self.device:
+            raise ValueError("k and v must be [batch, n_kv_heads, tokens, head_dim] on the cache's device")
+        return HackKv4Rows(_dtype_of(k), k.shape[2], _strides_of(k, "k"), _strides_of(v, "v"))
+
+    def hack_kv4_append(self, k, v, lens, new_lens=None, stream=None) -> None:
+        args = _cached(self._key("rows", _key(k, v, lens, new_lens)), lambda: self._rows(k, v, lens, new_lens))
+        status = _invoke(_KV4_APPEND, self._address, args, k, v, lens, new_lens, stream)
+        if status:
+            _check(status)
+
+    def hack_kv4_read(self, k_out, v_out, first, stream=None) -> None:
+        args = _cached(self._key("rows", _key(k_out, v_out, first, None)), lambda: self._rows(k_out, v_out, first, None))
+        status = _invoke(_KV4_READ, self._address, args, k_out, v_out, first, stream)
+        if status:
+            _check(status)
+
+    def _attend(self, q, out, lens, max_len, new_lens, appended, causal, n_sink, window, sm_scale, workspace_bytes):
+        self._lengths(lens, self.batch * self.n_kv_heads, "lens")
+        self._lengths(new_lens, self.batch, "new_lens")
+        _same("hack_kv4_attend", q, out)
+        if tuple(q.shape) != tuple(out.shape) or len(q.shape) != 4 or q.shape[0] != self.batch or q.shape[3] != self.head_dim or \
+                q.get_device() != self.device:
+            raise ValueError("q and out must be [batch, heads, tokens, head_dim] on the cache's device")
+        return HackKv4Attend(_dtype_of(q), q.shape[1], q.shape[2], max_len, int(appended), int(causal), window, n_sink, sm_scale, 0,
+                             workspace_bytes, _strides_of(q, "q"), _strides_of(out, "out"))
+
+    def hack_kv4_workspace(self, q, max_len: int, causal: bool = False, n_sink: int = 0, window: int = 0, appended: bool = False) -> int:
+        """Bytes of the workspace that hack_kv4_attend needs for queries of this shape and type."""
+        need = C.c_size_t()
+        args = self._attend(q, q, None, max_len, None, appended, causal, n_sink, window, 0.0, 0)
+        _check(lib.hack_kv4_workspace(self._address, C.addressof(args), C.byref(need)))
+        return need.value
+
+    def hack_kv4_attend(self, q, out, lens, max_len: int, workspace=None, new_lens=None, appended: bool = False, causal: bool = False,
+                        n_sink: int = 0, window: int = 0, sm_scale: float = 0.0, stream=None) -> None:
+        """q, out: [batch, heads, tokens, head_dim].  workspace: a uint8 tensor of hack_kv4_workspace bytes, or None where that
+        is 0."""
+        room = 0 if workspace is None else workspace.numel() * workspace.element_size()
+        args = _cached(self._key(max_len, appended, causal, n_sink, window, sm_scale, room, _key(q, out, lens, new_lens)),
+                       lambda: self._attend(q, out, lens, max_len, new_lens, appended, causal, n_sink, window, sm_scale, room))
+        status = _invoke(_KV4_ATTEND, self._address, args, q, out, lens, new_lens, workspace if room else None, stream)
+        if status:
+            _check(status)
+
+
 class HackCache:
     """Owner of one hack_cache_t.  Methods mirror the C entry points of the same name."""
 
@@ -427,6 +529,20 @@ class HackCache:
 
     def hack_scale_step_host(self, layer, scale, q, k, v, out, stream=None) -> None:
         _check(_call(_SCALE_STEP_HOST, self._address, layer, scale, q, k, v, out, stream))
+
+    def hack_scale_step_qkv(self, layer, scale, plan: Optional[HackRopePlan], q, k, v, out, positions, norm: int = HACK_NORM_RMS,
+                            eps: float = 1e-6, q_weight=None, k_weight=None, q_gain=None, k_gain=None, stream=None) -> None:
+        """hack_qk_norm_rope into buffers of the cache, then hack_scale_step."""
+        args = _cached((None if plan is None else (plan.axes, plan.head_dim), norm, eps, "step",
+                        _key(q, k, v, positions, q_weight, k_weight, q_gain, k_gain)),
+                       lambda: _qkv_args(plan, q, k, v, q, k, v, positions, norm, eps, q_weight, k_weight, q_gain, k_gain))
+        _check(lib.hack_scale_step_qkv(self._h, layer, scale, None if plan is None else C.addressof(plan), args, _ptr(q), _ptr(k),
+                                       _ptr(v), _ptr(positions), _ptr(q_weight), _ptr(k_weight), _ptr(q_gain), _ptr(k_gain), _ptr(out),
+                                       _ptr(stream)))
+
+    def hack_store_kv4(self, layer: int, kv4: HackKv4, lens, stream=None) -> None:
+        kv4._lengths(lens, self.batch * self.n_heads, "lens")
+        _check(lib.hack_store_kv4(self._h, layer, kv4._address, _ptr(lens), _ptr(stream)))
 
     def hack_get_lengths(self, layer: int):
         n = self.batch * self.n_heads

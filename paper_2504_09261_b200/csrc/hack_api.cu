@@ -9,8 +9,9 @@
 #include <new>
 #include <utility>
 
-#include "device_scope.h"
+#include "entry_checks.h"
 #include "hack_internal.h"
+#include "kv4.cuh"
 
 namespace hack {
 
@@ -153,6 +154,7 @@ struct hack_cache {
   cudaStream_t h2d_stream = nullptr, d2h_stream = nullptr;
   cudaEvent_t ev_in[kHostSlots] = {}, ev_step[kHostSlots] = {}, ev_out[kHostSlots] = {};
   uint64_t host_calls = 0;
+  unsigned char* prepared[3] = {};              // hack_scale_step_qkv: q, k, v of the step, made by its first call
   size_t reserved_bytes = 0, peak_bytes = 0;
   long long live_rows = 0;                      // stored (batch, head) rows over all layers
   uint64_t launches = 0;
@@ -579,6 +581,7 @@ hack_status_t hack_free_cache(hack_cache_t* c) {
     if (c->ev_step[sl]) cudaEventDestroy(c->ev_step[sl]);
     if (c->ev_out[sl]) cudaEventDestroy(c->ev_out[sl]);
   }
+  for (unsigned char* t : c->prepared) cudaFree(t);
   if (c->h2d_stream) cudaStreamDestroy(c->h2d_stream);
   if (c->d2h_stream) cudaStreamDestroy(c->d2h_stream);
   for (cudaEvent_t e : c->ev_pool) cudaEventDestroy(e);
@@ -963,6 +966,65 @@ hack_status_t hack_scale_step_host(hack_cache_t* c, int32_t layer, int32_t scale
   HACK_CUDA(cudaStreamWaitEvent(st, c->ev_out[sl], 0));
   ++c->host_calls;
   return HACK_OK;
+}
+
+hack_status_t hack_scale_step_qkv(hack_cache_t* c, int32_t layer, int32_t scale, const hack_rope_plan_t* plan,
+                                  const hack_qkv_args_t* args, const void* q, const void* k, const void* v,
+                                  const void* positions, const float* q_weight, const float* k_weight, const float* q_gain,
+                                  const float* k_gain, void* out, void* stream) {
+  hack_status_t s = check_step(c, layer, scale, 0);
+  if (s != HACK_OK) return s;
+  if (!args || !q || !k || !v || !out) return fail(HACK_ERR_INVALID_ARG, "args, q, k, v or out is NULL");
+  if (misaligned(out)) return fail(HACK_ERR_INVALID_ARG, "buffers must be 16-byte aligned");
+  const hack_config_t& g = c->cfg;
+  hack_qkv_args_t a = *args;
+  if (a.batch != g.batch || a.n_heads != g.n_heads || a.n_kv_heads != g.n_heads || a.n_tokens != c->n_tok[scale] ||
+      a.head_dim != g.head_dim || a.dtype != g.dtype || a.device != g.device)
+    return fail(HACK_ERR_INVALID_ARG, "args do not describe this scale of this cache");
+  HACK_ON_DEVICE(c);
+  const size_t full = (size_t)g.batch * g.n_heads * c->limits.max_new * g.head_dim * c->elt;
+  if (!c->prepared[0]) {
+    cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+    HACK_CUDA(cudaStreamIsCapturing((cudaStream_t)stream, &capturing));
+    if (capturing != cudaStreamCaptureStatusNone)
+      return fail(HACK_ERR_STATE, "the first hack_scale_step_qkv of a cache allocates: make it outside any stream capture");
+    unsigned char* t[3] = {};
+    cudaError_t e = cudaSuccess;
+    for (int i = 0; i < 3 && e == cudaSuccess; ++i) e = cudaMalloc(&t[i], full);
+    if (e != cudaSuccess) {
+      set_error(std::string("buffers of the prepared step: ") + cudaGetErrorString(e));
+      cudaGetLastError();
+      for (unsigned char* x : t) cudaFree(x);
+      return e == cudaErrorMemoryAllocation ? HACK_ERR_OOM : HACK_ERR_CUDA;
+    }
+    for (int i = 0; i < 3; ++i) c->prepared[i] = t[i];
+  }
+  const long long n = a.n_tokens, d = g.head_dim;
+  a.q_out = a.k_out = a.v_out = hack_strides_t{g.n_heads * n * d, n * d, d};
+  s = hack_qk_norm_rope(plan, &a, q, k, v, c->prepared[0], c->prepared[1], c->prepared[2], positions, q_weight, k_weight, q_gain,
+                        k_gain, stream);
+  if (s != HACK_OK) return s;
+  ++c->launches;
+  return hack_scale_step(c, layer, scale, c->prepared[0], c->prepared[1], c->prepared[2], out, stream);
+}
+
+hack_status_t hack_store_kv4(hack_cache_t* c, int32_t layer, const hack_kv4_t* kv, const int32_t* lens, void* stream) {
+  if (!c) return fail(HACK_ERR_INVALID_ARG, "cache is NULL");
+  if (c->poisoned) return fail(HACK_ERR_STATE, "an earlier step failed half way; call hack_reset before the next image");
+  if (layer < 0 || layer >= c->cfg.n_layers) return fail(HACK_ERR_INVALID_ARG, "layer out of range");
+  const hack_status_t s = hack::kv4_check(kv);
+  if (s != HACK_OK) return s;
+  if (kv->batch != c->cfg.batch || kv->n_kv_heads != c->cfg.n_heads || kv->head_dim != c->cfg.head_dim || kv->device != c->cfg.device)
+    return fail(HACK_ERR_INVALID_ARG, "the 4-bit cache has another batch, heads, head_dim or device");
+  if (!lens) return fail(HACK_ERR_INVALID_ARG, "lens is NULL");
+  HACK_ON_DEVICE(c);
+  const LayerState& ls = c->layers[layer];
+  hack_step_info_t p{};
+  p.kept_s = ls.len[0];
+  p.kept_c = ls.len[1];
+  const hack_status_t r = hack::launch_store_kv4(make_args(c, layer, 0, p), c->cfg.dtype, kv, lens, (cudaStream_t)stream);
+  if (r == HACK_OK) ++c->launches;
+  return r;
 }
 
 hack_status_t hack_get_lengths(const hack_cache_t* c, int32_t layer, int32_t* host_out) {

@@ -14,7 +14,7 @@
 #include <cmath>
 #include <string>
 
-#include "device_scope.h"
+#include "entry_checks.h"
 #include "hack_internal.h"
 
 namespace hack {
@@ -265,23 +265,9 @@ bool bad(const char* text) {
   return true;
 }
 
-// A [batch, heads, tokens, head_dim] tensor whose rows start on 16-byte boundaries; one that is written has a place of its
-// own for every row.
 bool bad_view(const void* ptr, const hack_strides_t& s, int batch, int heads, int tokens, int head_dim, int elt, bool written) {
-  if (!ptr) return bad("a tensor is NULL");
-  const long long bytes = elt;
-  if ((reinterpret_cast<uintptr_t>(ptr) & 15) || (s.batch * bytes) % 16 || (s.head * bytes) % 16 || (s.token * bytes) % 16)
-    return bad("rows must start on 16-byte boundaries");
-  if (!written) return false;
-  struct Dim { long long stride, n; } d[3] = {{s.batch, batch}, {s.head, heads}, {s.token, tokens}};
-  std::sort(d, d + 3, [](const Dim& x, const Dim& y) { return x.stride < y.stride; });
-  long long extent = head_dim;                // elements that the inner dimensions take
-  for (const Dim& x : d) {
-    if (x.n == 1) continue;
-    if (x.stride < extent) return bad("rows of an output overlap");
-    extent += x.stride * (x.n - 1);
-  }
-  return false;
+  const char* text = view_error(ptr, s, batch, heads, tokens, head_dim, elt, written);
+  return text ? bad(text) : false;
 }
 
 bool bad_plan(const hack_rope_plan_t* plan, int head_dim) {

@@ -81,3 +81,73 @@ def test_qk_norm_rope_refuses(hb, change, status):
     p = None if "plan" in change and change["plan"] is None else C.addressof(plan)
     assert bd.lib.hack_qk_norm_rope(p, C.addressof(args), *ptr.values(), None, None, None, None, None) == status
     assert hb.hack_last_error()
+
+
+def _kv4(**change):
+    from paper_2504_09261_b200 import binding as bd
+    f = dict(device=0, batch=2, n_kv_heads=3, head_dim=128, cap=50, reserved=0, row_off=None, k_codes=4096, v_codes=8192, k_scales=12288,
+             v_scales=16384)
+    f.update(change)
+    return bd.HackKv4Planes(*f.values())
+
+
+@pytest.mark.parametrize("change,status", [(dict(head_dim=32), 2), (dict(batch=0), 1), (dict(n_kv_heads=-1), 1), (dict(cap=0), 1), (dict(device=-2), 1),
+                                           (dict(k_codes=None), 1), (dict(v_scales=16392), 1), (dict(batch=1 << 20, n_kv_heads=1 << 12), 1)])
+def test_kv4_planes_refused(hb, change, status):
+    from paper_2504_09261_b200 import binding as bd
+    kv, rows = _kv4(**change), bd.HackKv4Rows(1, 4, bd.HackStrides(1536, 512, 128), bd.HackStrides(1536, 512, 128))
+    at = bd.HackKv4Attend(1, 3, 1, 10, 0, 0, 0, 0, 0.0, 0, 0, bd.HackStrides(384, 128, 128), bd.HackStrides(384, 128, 128))
+    k, r, a = C.addressof(kv), C.addressof(rows), C.addressof(at)
+    need = C.c_size_t()
+    assert bd.lib.hack_kv4_append(k, r, 4096, 4096, 4096, None, None) == status
+    assert bd.lib.hack_kv4_read(k, r, 4096, 4096, 4096, None) == status
+    assert bd.lib.hack_kv4_workspace(k, a, C.byref(need)) == status
+    assert bd.lib.hack_kv4_attend(k, a, 4096, 8192, 4096, None, None, None) == status
+    assert bd.lib.hack_kv4_append(None, r, 4096, 4096, 4096, None, None) == 1
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(dtype=3), 2), (dict(n_tokens=-1), 1), (dict(k=(1536, 512, 100)), 1), (dict(v=(1536, 512, 64)), 1)])
+def test_kv4_rows_refused(hb, change, status):
+    from paper_2504_09261_b200 import binding as bd
+    kv = _kv4()
+    rows = bd.HackKv4Rows(change.get("dtype", 1), change.get("n_tokens", 4), bd.HackStrides(*change.get("k", (1536, 512, 128))),
+                          bd.HackStrides(*change.get("v", (1536, 512, 128))))
+    k, r = C.addressof(kv), C.addressof(rows)
+    assert bd.lib.hack_kv4_read(k, r, 4096, 8192, 4096, None) == status           # (64 apart: rows of an output would overlap)
+    for call in ((k, r, None, 4096, 4096), (k, r, 4096, None, 4096), (k, r, 4096, 4096, None), (k, None, 4096, 4096, 4096), (k, r, 4100, 4096, 4096)):
+        assert bd.lib.hack_kv4_append(*call, None, None) == (1 if change.get("dtype", 1) == 1 or call[1] is None else 2)
+    none = bd.HackKv4Rows(1, 0)
+    assert bd.lib.hack_kv4_append(k, C.addressof(none), None, None, None, None, None) == 0
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(dtype=3), 2), (dict(n_heads=4), 1), (dict(n_heads=0), 1), (dict(n_queries=-1), 1), (dict(max_len=-1), 1), (dict(window=-1), 1),
+    (dict(n_sink=-1), 1), (dict(sm_scale=-1.0), 1), (dict(sm_scale=float("nan")), 1), (dict(n_queries=1 << 30), 1)])
+def test_kv4_attend_refused(hb, change, status):
+    from paper_2504_09261_b200 import binding as bd
+    f = dict(dtype=1, n_heads=6, n_queries=1, max_len=10, appended=0, causal=0, window=0, n_sink=0, sm_scale=0.0, reserved=0, workspace_bytes=0)
+    f.update(change)
+    args = bd.HackKv4Attend(*f.values(), bd.HackStrides(768, 128, 128), bd.HackStrides(768, 128, 128))
+    kv = _kv4()
+    k, a, need = C.addressof(kv), C.addressof(args), C.c_size_t()
+    assert bd.lib.hack_kv4_workspace(k, a, C.byref(need)) == status
+    assert bd.lib.hack_kv4_attend(k, a, 4096, 8192, 4096, None, None, None) == status
+    assert hb.hack_last_error()
+
+
+def test_kv4_attend_refuses_tensors(hb):
+    from paper_2504_09261_b200 import binding as bd
+    kv = _kv4()
+    good = dict(dtype=1, n_heads=6, n_queries=1, max_len=10, appended=0, causal=0, window=0, n_sink=0, sm_scale=0.0, reserved=0, workspace_bytes=0)
+
+    def call(q=4096, out=8192, lens=4096, strides=(768, 128, 128), out_strides=(768, 128, 128), n=1):
+        args = bd.HackKv4Attend(*{**good, "n_queries": n}.values(), bd.HackStrides(*strides), bd.HackStrides(*out_strides))
+        return bd.lib.hack_kv4_attend(C.addressof(kv), C.addressof(args), q, out, lens, None, None, None)
+
+    assert call(q=None) == call(out=None) == call(lens=None) == call(q=4104) == call(strides=(768, 129, 128)) == 1
+    assert call(out_strides=(0, 128, 128)) == call(out_strides=(768, 64, 128)) == 1
+    assert call(n=0, q=None, out=None, lens=None) == 0
+    assert bd.lib.hack_kv4_attend(C.addressof(kv), None, 4096, 8192, 4096, None, None, None) == 1
+    assert bd.lib.hack_store_kv4(None, 0, C.addressof(kv), 4096, None) == 1
+    assert bd.lib.hack_scale_step_qkv(None, 0, 0, *([None] * 12)) == 1
