@@ -418,7 +418,8 @@ typedef struct {
   int32_t window, n_sink;        /* window > 0: of the rows up to its position a query sees the last `window` (itself
                                     counted) and the first n_sink */
   float sm_scale;                /* 0 selects 1 / sqrt(head_dim) */
-  int32_t reserved;
+  int32_t wait_polls;            /* limit of the device-side waits, in polls of a barrier; 0: most of a second.  For tests: a
+                                    limit of 1 makes the first wait that is not already satisfied give up */
   int64_t workspace_bytes;       /* size of the workspace given */
   hack_strides_t q, out;
 } hack_kv4_attend_t;
@@ -429,6 +430,10 @@ HACK_API hack_status_t hack_kv4_workspace(const hack_kv4_t* kv, const hack_kv4_a
  * calls that may overlap on the GPU need workspaces of their own. */
 HACK_API hack_status_t hack_kv4_attend(const hack_kv4_t* kv, const hack_kv4_attend_t* args, const void* q, void* out,
                                        const int32_t* lens, const int32_t* new_lens, void* workspace, void* stream);
+
+/* Synchronises `stream`, then reports whether a bounded device-side wait of hack_kv4_attend on this device gave up since the
+ * last call: HACK_OK or HACK_ERR_TIMEOUT (what that call wrote is undefined). */
+HACK_API hack_status_t hack_kv4_poll_status(int32_t device, void* stream);
 
 /* Text of the calling thread's last error; never NULL. */
 HACK_API const char* hack_last_error(void);

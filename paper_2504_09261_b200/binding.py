@@ -36,7 +36,7 @@ EXPORTS = (
     "hack_launch_count", "hack_stage_timing", "hack_stage_times", "hack_poll_status", "hack_set_wait_limit",
     "hack_debug_build", "hack_debug_check", "hack_last_error",
     "hack_rope_plan", "hack_rope", "hack_qk_norm_rope", "hack_scale_step_qkv", "hack_kv4_append", "hack_kv4_read",
-    "hack_store_kv4", "hack_kv4_workspace", "hack_kv4_attend",
+    "hack_store_kv4", "hack_kv4_workspace", "hack_kv4_attend", "hack_kv4_poll_status",
 )
 
 
@@ -95,7 +95,7 @@ class HackKv4Rows(C.Structure):
 
 class HackKv4Attend(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("dtype", "n_heads", "n_queries", "max_len", "appended", "causal", "window", "n_sink")] + [
-        ("sm_scale", C.c_float), ("reserved", C.c_int32), ("workspace_bytes", C.c_int64), ("q", HackStrides), ("out", HackStrides)]
+        ("sm_scale", C.c_float), ("wait_polls", C.c_int32), ("workspace_bytes", C.c_int64), ("q", HackStrides), ("out", HackStrides)]
 
 
 class HackError(RuntimeError):
@@ -149,6 +149,7 @@ def _load() -> C.CDLL:
     sigs["hack_store_kv4"] = [vp, i32, vp, vp, vp]
     sigs["hack_kv4_workspace"] = [vp, vp, C.POINTER(C.c_size_t)]
     sigs["hack_kv4_attend"] = [vp] * 8
+    sigs["hack_kv4_poll_status"] = [i32, vp]
     for name, args in sigs.items():
         fn = getattr(lib, name)
         fn.argtypes = args
@@ -439,6 +440,9 @@ class HackKv4:
         status = _invoke(_KV4_ATTEND, self._address, args, q, out, lens, new_lens, workspace if room else None, stream)
         if status:
             _check(status)
+
+    def hack_kv4_poll_status(self, stream=None) -> None:
+        _check(lib.hack_kv4_poll_status(self.device, _ptr(stream)))
 
 
 class HackCache:

@@ -33,6 +33,8 @@ constexpr int kRows = 16;                    // query rows of a CTA
 constexpr int kChunk = 32;                   // stored rows of a turn of a warp
 constexpr int kStages = 3;
 constexpr float kRaise = 16.f;               // log2 by which a logit may exceed the reference maximum
+constexpr int kTcRows = 48;                  // bf16: from so many query rows of a stored head on, tiles of 128 on the tensor cores
+constexpr uint32_t kWaitPolls = 1u << 24;    // of a wait in that kernel: a large part of a second at least
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool live) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
@@ -367,42 +369,48 @@ __global__ void __launch_bounds__(kThreads) kv4_attend_kernel(const __grid_const
   }
 }
 
-// Partial results of the splits: one CTA of D / 4 threads per row of 16.
+// Partial results of the splits added up: D / 4 threads for a query row.
 template <int D, bool F32>
 __global__ void __launch_bounds__(256) kv4_combine_kernel(const __grid_constant__ Kv4AttendParams p) {
   pdl_wait();
   constexpr int LANES = D / 4, PER = 256 / LANES;
   const long long index = (long long)blockIdx.x * PER + threadIdx.x / LANES;
-  const int unit = (int)(index / kRows), row = (int)(index - (long long)unit * kRows), d = (threadIdx.x % LANES) * 4;
+  const int unit = (int)(index / p.tile_rows), row = (int)(index - (long long)unit * p.tile_rows), d = (threadIdx.x % LANES) * 4;
   if (unit >= p.units) return;
   const int head = unit / p.tiles, tile = unit - head * p.tiles;
   const int b = head / p.kv_heads, kvh = head - b * p.kv_heads;
   const int nq = p.new_lens ? min(max(p.new_lens[b], 0), p.n_queries) : p.n_queries;
-  if (tile * kRows + row >= nq * p.group) return;
-  const float* part = p.partial + (long long)unit * p.splits * (kRows * (D + 2));
+  const int m = tile * p.tile_rows + row;
+  if (m >= nq * p.group) return;
+  const long long step = (long long)p.tile_rows * (D + 2);
+  const float* part = p.partial + (long long)unit * p.splits * step;
+  const float* stats = part + (long long)p.tile_rows * D + 2 * row;
   float mx = kNoLogit;
-  for (int s = 0; s < p.splits; ++s) mx = fmaxf(mx, part[(long long)s * (kRows * (D + 2)) + kRows * D + 2 * row]);
+  for (int s = 0; s < p.splits; ++s) mx = fmaxf(mx, stats[s * step]);
   float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
   float total = 0.f;
   for (int s = 0; s < p.splits; ++s) {
-    const float* x = part + (long long)s * (kRows * (D + 2));
-    const float f = ex2((x[kRows * D + 2 * row] - mx) * p.scale_log2);
-    const float4 v = *reinterpret_cast<const float4*>(x + row * D + d);
-    total += f * x[kRows * D + 2 * row + 1];
+    const float f = ex2((stats[s * step] - mx) * p.scale_log2);
+    const float4 v = *reinterpret_cast<const float4*>(part + s * step + (long long)row * D + d);
+    total += f * stats[s * step + 1];
     sum.x = fmaf(f, v.x, sum.x); sum.y = fmaf(f, v.y, sum.y); sum.z = fmaf(f, v.z, sum.z); sum.w = fmaf(f, v.w, sum.w);
   }
-  kv4_store<F32>(p, b, kvh, tile * kRows + row, d, sum, total);
+  kv4_store<F32>(p, b, kvh, m, d, sum, total);
 }
 
 template <int D, bool F32>
-int launch_few(const Kv4AttendParams& p, cudaStream_t st) {
-  constexpr size_t smem = smem_bytes<D, F32>();
-  if (!allow_dynamic_smem(kv4_attend_kernel<D, F32>, smem)) return -1;
-  const int y = std::min(p.units, 32768);
-  launch_k(kv4_attend_kernel<D, F32>, dim3(p.splits, y, (p.units + y - 1) / y), dim3(kThreads), smem, st, p);
+int launch_attend(const Kv4AttendParams& p, cudaStream_t st) {
+  if (p.tile_rows == kRows) {
+    constexpr size_t smem = smem_bytes<D, F32>();
+    if (!allow_dynamic_smem(kv4_attend_kernel<D, F32>, smem)) return -1;
+    const int y = std::min(p.units, 32768);
+    launch_k(kv4_attend_kernel<D, F32>, dim3(p.splits, y, (p.units + y - 1) / y), dim3(kThreads), smem, st, p);
+  } else if (launch_kv4_attend_tc(p, D, st) < 0) {
+    return -1;
+  }
   if (p.splits > 1) {
     constexpr int PER = 256 / (D / 4);
-    launch_k(kv4_combine_kernel<D, F32>, dim3((unsigned)(((long long)p.units * kRows + PER - 1) / PER)), dim3(256), 0, st, p);
+    launch_k(kv4_combine_kernel<D, F32>, dim3((unsigned)(((long long)p.units * p.tile_rows + PER - 1) / PER)), dim3(256), 0, st, p);
   }
   return launched(1);
 }
@@ -420,6 +428,7 @@ hack_status_t check_attend(const hack_kv4_t* kv, const hack_kv4_attend_t* a) {
   if (a->n_heads < 1 || a->n_heads % kv->n_kv_heads) return invalid("n_heads must be a multiple of n_kv_heads");
   if (a->n_queries < 0 || a->max_len < 0) return invalid("n_queries and max_len must not be negative");
   if (a->window < 0 || a->n_sink < 0) return invalid("window and n_sink must not be negative");
+  if (a->wait_polls < 0) return invalid("wait_polls must not be negative");
   if (!(a->sm_scale >= 0.f) || !std::isfinite(a->sm_scale)) return invalid("sm_scale must be finite and non-negative");
   if ((long long)a->n_queries * (a->n_heads / kv->n_kv_heads) > 0x3fffffffll) return invalid("too many queries");
   return HACK_OK;
@@ -436,16 +445,26 @@ hack_status_t plan(const hack_kv4_t* kv, const hack_kv4_attend_t* a, Kv4AttendPa
   p.n_sink = a->window > 0 ? a->n_sink : 0;
   p.appended = a->appended != 0;
   const int heads = kv->batch * kv->n_kv_heads, rows = a->n_queries * p.group;
-  p.tiles = (rows + kRows - 1) / kRows;
+  const bool tc = a->dtype == HACK_BF16 && rows >= kTcRows;
+  p.tile_rows = tc ? 128 : kRows;
+  p.tiles = (rows + p.tile_rows - 1) / p.tile_rows;
   const long long units = (long long)heads * p.tiles;
   if (units > 0x3fffffffll) { set_error("more query rows than a launch has places for"); return HACK_ERR_UNSUPPORTED; }
   p.units = (int)units;
   // rows that a tile of queries walks at most
   long long walked = p.max_len;
   if (p.window > 0) walked = std::min<long long>(walked, (long long)p.window + p.n_sink + p.n_queries);
-  const long long turns = (walked + kChunk * kWarps - 1) / (kChunk * kWarps);
-  p.splits = (int)std::max<long long>(1, std::min<long long>(turns / 2, 4ll * sm_count() / units));
-  workspace = p.splits > 1 ? (size_t)p.units * p.splits * kRows * (kv->head_dim + 2) * 4 : 0;
+  const int sms = sm_count();
+  if (tc) {
+    p.tiles_per_cta = units <= sms ? 1 : 2;
+    const long long ctas = (long long)heads * ((p.tiles + p.tiles_per_cta - 1) / p.tiles_per_cta);
+    p.splits = (int)std::max<long long>(1, std::min<long long>((walked + 127) / 128 / 4, sms / ctas));
+  } else {
+    const long long turns = (walked + kChunk * kWarps - 1) / (kChunk * kWarps);
+    p.splits = (int)std::max<long long>(1, std::min<long long>(turns / 2, 4ll * sms / units));
+  }
+  p.wait_polls = a->wait_polls > 0 ? (uint32_t)a->wait_polls : kWaitPolls;
+  workspace = p.splits > 1 ? (size_t)p.units * p.splits * p.tile_rows * (kv->head_dim + 2) * 4 : 0;
   return HACK_OK;
 }
 
@@ -489,10 +508,11 @@ extern "C" hack_status_t hack_kv4_attend(const hack_kv4_t* kv, const hack_kv4_at
   p.q_stride = a.q;
   p.out_stride = a.out;
   p.scale_log2 = (a.sm_scale > 0.f ? a.sm_scale : 1.f / std::sqrt((float)kv->head_dim)) * 1.4426950408889634f;
+  p.out_sectors = reinterpret_cast<uintptr_t>(out) % 32 == 0 && a.out.batch * elt % 32 == 0 && a.out.head * elt % 32 == 0 && a.out.token * elt % 32 == 0;
   p.partial = static_cast<float*>(workspace);
   cudaStream_t st = (cudaStream_t)stream;
   int n;
-  if (kv->head_dim == 64) n = a.dtype == HACK_F32 ? launch_few<64, true>(p, st) : launch_few<64, false>(p, st);
-  else n = a.dtype == HACK_F32 ? launch_few<128, true>(p, st) : launch_few<128, false>(p, st);
+  if (kv->head_dim == 64) n = a.dtype == HACK_F32 ? launch_attend<64, true>(p, st) : launch_attend<64, false>(p, st);
+  else n = a.dtype == HACK_F32 ? launch_attend<128, true>(p, st) : launch_attend<128, false>(p, st);
   return n < 0 ? HACK_ERR_CUDA : HACK_OK;
 }

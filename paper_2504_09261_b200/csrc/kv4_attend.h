@@ -10,15 +10,22 @@ struct Kv4AttendParams {
   int kv_heads, group;              // group: query heads of a stored head
   int n_queries, max_len;
   int causal, window, n_sink, appended;
+  int tile_rows;                    // query rows of a tile: 16, or 128 on the tensor cores
   int tiles, units, splits;         // tiles of query rows of a stored head, all of them, CTAs that share the rows of one
+  int tiles_per_cta;                // tensor cores: 1 or 2
+  int out_sectors;                  // rows of the output start on 32-byte boundaries
+  uint32_t wait_polls;              // limit of a wait
   float scale_log2;                 // sm_scale * log2(e)
   const int32_t* lens;
   const int32_t* new_lens;
   const void* q;
   void* out;
   hack_strides_t q_stride, out_stride;
-  float* partial;                   // [units][splits]: [16][D] outputs, [16][2] reference maximum and sum
+  float* partial;                   // [units][splits]: [tile_rows][D] outputs, [tile_rows][2] reference maximum and sum
 };
+
+// The tensor-core kernel (bf16); partial results where splits > 1.
+int launch_kv4_attend_tc(const Kv4AttendParams& p, int head_dim, cudaStream_t st);
 
 // Rows of a head that its queries may see: [0, sink_end) and [lo, hi).  Every row of a tile sees all of [all_lo, all_hi), and those of
 // [0, all_sink).

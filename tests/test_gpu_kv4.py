@@ -315,6 +315,88 @@ def test_two_streams_with_workspaces_of_their_own(hb):
     assert torch.equal(outs[0], alone) and torch.equal(outs[1], alone)
 
 
+# ------------------------------------------------------------------ many queries: tiles of 128 rows on the tensor cores
+MANY = [  # dim, batch, kv_heads, group, tokens, cap
+    (128, 1, 1, 1, 48, 100), (64, 1, 1, 1, 128, 128), (128, 1, 2, 1, 129, 300), (64, 2, 3, 3, 43, 257), (128, 1, 1, 4, 100, 1000),
+    (64, 1, 2, 1, 513, 640), (128, 3, 2, 2, 65, 40), (64, 1, 1, 1, 300, 5000), (128, 1, 1, 8, 60, 9000), (128, 2, 80, 1, 130, 200),
+    (64, 2, 80, 1, 257, 131),
+]
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dim,batch,kv_heads,group,tokens,cap", MANY)
+def test_attend_many_queries(hb, causal, dim, batch, kv_heads, group, tokens, cap):
+    n = batch * kv_heads
+    lens = [cap] + [(i * 101) % (cap + 1) for i in range(1, n)]
+    _check(hb, _gen(cap), torch.bfloat16, dim, batch, kv_heads, group, tokens, cap, lens, causal=causal)
+
+
+@pytest.mark.parametrize("length", [0, 1, 31, 32, 33, 127, 128, 129, 255, 256, 257, 384, 511])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_attend_many_queries_lengths(hb, dim, length):
+    _check(hb, _gen(length), torch.bfloat16, dim, 1, 2, 1, 140, 512, [length, 512 - length], causal=dim == 64)
+    _check(hb, _gen(length), torch.bfloat16, dim, 1, 2, 3, 100, 512, [length, 512 - length], causal=dim == 128)
+
+
+@pytest.mark.parametrize("tokens", [60, 200])
+@pytest.mark.parametrize("window,n_sink", [(1, 0), (1, 1), (7, 4), (128, 0), (100, 140), (300, 3), (1000, 5)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_attend_many_queries_window(hb, tokens, window, n_sink, causal):
+    _check(hb, _gen(window), torch.bfloat16, 64, 1, 3, 2, tokens, 700, [700, 190, 12], causal=causal, window=window, n_sink=n_sink)
+    _check(hb, _gen(window), torch.bfloat16, 128, 1, 1, 1, tokens, 700, [611], causal=causal, window=window, n_sink=n_sink)
+
+
+def test_attend_many_queries_padded_and_limits(hb):
+    g, dt = _gen(22), torch.bfloat16
+    _check(hb, g, dt, 128, 3, 2, 2, 150, 400, [10, 94, 50, 99, 0, 7], new_lens=[150, 70, 0], appended=True, causal=True)
+    _check(hb, g, dt, 64, 2, 2, 1, 300, 500, [-3, 2 ** 31 - 1, 50, 0], new_lens=[-1, 900], appended=True, causal=True)
+    _check(hb, g, dt, 64, 2, 2, 1, 64, 500, [2 ** 31 - 1, -2 ** 31, 49, 1], max_len=300)
+    _check(hb, g, dt, 64, 1, 1, 1, 64, 50, [20], max_len=0)
+    _check(hb, g, dt, 128, 1, 3, 1, 70, 140, [140, 3, 121], row_off=torch.tensor([281, 0, 140], dtype=torch.int64, device="cuda"), rows=422, q_layout="head")
+    _check(hb, g, dt, 128, 1, 3, 1, 70, 140, [140, 3, 21], sm_scale=2.5, q_size=3.0)
+
+
+def test_rows_whose_output_starts_on_16_bytes_only(hb):
+    """bf16 rows 16 but not 32 bytes apart from a sector's start."""
+    g, dim, cap, n = _gen(23), 64, 300, 130
+    planes = Planes(cap, dim)
+    planes.randomise(g)
+    kv4 = planes.handle(hb, 1, 1, cap)
+    wide = torch.full((1, 1, n, dim + 8), 5.0, dtype=torch.bfloat16, device="cuda")
+    q = torch.randn(1, 1, n, dim + 8, generator=g, device="cuda").to(torch.bfloat16)[..., 8:]
+    kv4.hack_kv4_attend(q, wide[..., 8:], _ints(cap), cap, workspace=torch.empty(1 << 24, dtype=torch.uint8, device="cuda"))
+    want = ref.attend(q[0], ref.values(planes.k_codes, planes.k_scales), ref.values(planes.v_codes, planes.v_scales), cap, n, dim ** -0.5)
+    assert ((wide[0, ..., 8:].double() - want[0]).abs() <= ref.bound(*want, torch.bfloat16, dim, cap)).all()
+    assert (wide[..., :8] == 5.0).all()
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_a_wait_that_runs_out_is_reported(hb, dim):
+    from paper_2504_09261_b200 import binding as bd
+    import ctypes as C
+    g, cap, n = _gen(24), 2000, 300
+    planes = Planes(2 * cap, dim)
+    planes.randomise(g)
+    kv4 = planes.handle(hb, 1, 2, cap)
+    q = torch.randn(1, 2, n, dim, generator=g, device="cuda").to(torch.bfloat16)
+    out, good = torch.empty_like(q), torch.empty_like(q)
+    lens = _ints(cap, cap)
+    need = kv4.hack_kv4_workspace(q, cap)
+    work = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+    kv4.hack_kv4_attend(q, good, lens, cap, workspace=work)
+    kv4.hack_kv4_poll_status()
+    args = kv4._attend(q, out, lens, cap, None, False, False, 0, 0, 0.0, work.numel())
+    args.wait_polls = 1
+    assert bd.lib.hack_kv4_attend(kv4._address, C.addressof(args), q.data_ptr(), out.data_ptr(), lens.data_ptr(), None, work.data_ptr(), None) == 0
+    with pytest.raises(hb.HackError) as e:
+        kv4.hack_kv4_poll_status()
+    assert e.value.status == 6
+    kv4.hack_kv4_poll_status()                                    # reported once
+    kv4.hack_kv4_attend(q, out, lens, cap, workspace=work)        # and the next call is right
+    assert torch.equal(out, good)
+    kv4.hack_kv4_poll_status()
+
+
 # ------------------------------------------------------------------ together with the cache's steps
 @pytest.mark.parametrize("config", [0, 1])
 def test_from_projections_to_a_stored_cache(hb, config):

@@ -123,10 +123,10 @@ def test_kv4_rows_refused(hb, change, status):
 
 @pytest.mark.parametrize("change,status", [
     (dict(dtype=3), 2), (dict(n_heads=4), 1), (dict(n_heads=0), 1), (dict(n_queries=-1), 1), (dict(max_len=-1), 1), (dict(window=-1), 1),
-    (dict(n_sink=-1), 1), (dict(sm_scale=-1.0), 1), (dict(sm_scale=float("nan")), 1), (dict(n_queries=1 << 30), 1)])
+    (dict(n_sink=-1), 1), (dict(sm_scale=-1.0), 1), (dict(sm_scale=float("nan")), 1), (dict(n_queries=1 << 30), 1), (dict(wait_polls=-1), 1)])
 def test_kv4_attend_refused(hb, change, status):
     from paper_2504_09261_b200 import binding as bd
-    f = dict(dtype=1, n_heads=6, n_queries=1, max_len=10, appended=0, causal=0, window=0, n_sink=0, sm_scale=0.0, reserved=0, workspace_bytes=0)
+    f = dict(dtype=1, n_heads=6, n_queries=1, max_len=10, appended=0, causal=0, window=0, n_sink=0, sm_scale=0.0, wait_polls=0, workspace_bytes=0)
     f.update(change)
     args = bd.HackKv4Attend(*f.values(), bd.HackStrides(768, 128, 128), bd.HackStrides(768, 128, 128))
     kv = _kv4()
@@ -139,7 +139,7 @@ def test_kv4_attend_refused(hb, change, status):
 def test_kv4_attend_refuses_tensors(hb):
     from paper_2504_09261_b200 import binding as bd
     kv = _kv4()
-    good = dict(dtype=1, n_heads=6, n_queries=1, max_len=10, appended=0, causal=0, window=0, n_sink=0, sm_scale=0.0, reserved=0, workspace_bytes=0)
+    good = dict(dtype=1, n_heads=6, n_queries=1, max_len=10, appended=0, causal=0, window=0, n_sink=0, sm_scale=0.0, wait_polls=0, workspace_bytes=0)
 
     def call(q=4096, out=8192, lens=4096, strides=(768, 128, 128), out_strides=(768, 128, 128), n=1):
         args = bd.HackKv4Attend(*{**good, "n_queries": n}.values(), bd.HackStrides(*strides), bd.HackStrides(*out_strides))
