@@ -51,6 +51,10 @@ __device__ __forceinline__ uint32_t values2(uint32_t w, int shift, const Scale2&
   asm("lop3.b32 %0, %1, 0x000f000f, 0x43004300, 0xea;" : "=r"(x) : "r"(w >> shift));   // (w & mask) | magic
   return bf162_fma(x, s.s, s.off);
 }
+// x += the low, y += the high bf16 number of w
+__device__ __forceinline__ void add_bf162(float& x, float& y, uint32_t w) {
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tadd.rn.f32.bf16 %0, l, %0;\n\tadd.rn.f32.bf16 %1, h, %1;\n\t}" : "+f"(x), "+f"(y) : "r"(w));
+}
 #endif
 
 }  // namespace kv4

@@ -7,10 +7,13 @@
 // kv4_attend_kernel: few rows, or fp32.  A warp takes chunks of 32 stored rows through a ring of its own in shared memory
 // (cp.async, so that neither their place nor the end of a head has to be aligned); its lanes read the codes there in the
 // order of the matrix fragments - the order of the elements inside a product is free as long as both operands
-// have it - so that a value costs a shift, a mask and an FMA for two.  Softmax with a running maximum that is raised only when
-// a logit exceeds it by 2^16; a CTA's warps are merged in shared memory, CTAs that share the rows of a head (`splits`)
-// through partial results in the workspace, which kv4_combine_kernel adds up.
+// have it - so that a value costs a shift, a mask and an FMA for two.  The stored rows are the 16 rows of a product
+// and the queries its eight columns (K Q^T, then V^T P^T): one query, or the few that share a stored head, leave as little of it
+// empty as can be, and hold half the registers of the other way round.  Softmax with a running maximum that is
+// raised only when a logit exceeds it by 2^16; a CTA's warps are merged in shared memory, CTAs that share the rows of a head
+// (`splits`) through partial results in the workspace, which kv4_combine_kernel adds up.
 // fp32: queries and probabilities as sums of three bf16 numbers, which is all of their 24 bits.
+// kv4_attend_tc_kernel (kv4_attend_tc.cu): bf16, from kTcRows query rows on.
 #include <algorithm>
 #include <cmath>
 #include <string>
@@ -25,22 +28,18 @@ namespace {
 
 using namespace kv4;
 using ptx::ex2;
-using ptx::mma16816;
 using ptx::smem_u32;
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
-constexpr int kRows = 16;                    // query rows of a CTA
 constexpr int kChunk = 32;                   // stored rows of a turn of a warp
 constexpr int kStages = 3;
 constexpr float kRaise = 16.f;               // log2 by which a logit may exceed the reference maximum
 constexpr int kTcRows = 48;                  // bf16: from so many query rows of a stored head on, tiles of 128 on the tensor cores
 constexpr uint32_t kWaitPolls = 1u << 24;    // of a wait in that kernel: a large part of a second at least
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool live) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
-}
-template <int BYTES> __device__ __forceinline__ void cp_async_small(uint32_t dst, const void* src, bool live) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(live ? BYTES : 0) : "memory");
+template <int BYTES> __device__ __forceinline__ void cp_async(uint32_t dst, const void* src, int bytes) {
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -51,6 +50,17 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 }
 __device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+// D += A B, 16 x 8 x 16.  (Not volatile: the chains of independent products may be interleaved.)
+__device__ __forceinline__ void mma(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// An 8 x 8 matrix of 16-bit numbers in fragment order, transposed
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
 
 template <int D> struct Ring {
   static constexpr int kCodes = kChunk * D / 2, kScales = kChunk * D / 16;   // bytes of a chunk, of K or V
@@ -58,18 +68,23 @@ template <int D> struct Ring {
   static constexpr int kWarp = kStages * kStage;
 };
 // The ring, later the warps' outputs; fp32: the query's fragments behind it.
-template <int D, bool F32> constexpr size_t smem_bytes() {
-  constexpr size_t ring = (size_t)kWarps * Ring<D>::kWarp, merge = (size_t)kWarps * kRows * D * 4;
-  return (ring > merge ? ring : merge) + (F32 ? 3 * (D / 16) * 32 * 16 : 0);
+template <int D, bool F32, int NQ> constexpr size_t smem_bytes() {
+  constexpr size_t ring = (size_t)kWarps * Ring<D>::kWarp, merge = (size_t)kWarps * 8 * NQ * D * 4;
+  return (ring > merge ? ring : merge) + (F32 ? 3 * NQ * (D / 16) * 32 * 8 : 0);
 }
 
-template <int D, bool F32>
-__global__ void __launch_bounds__(kThreads) kv4_attend_kernel(const __grid_constant__ Kv4AttendParams p) {
-  constexpr int KS = D / 16;                 // k-steps of Q K^T, and a lane's 4 codes each
-  constexpr int NT = D / 8;                  // column tiles of the output
+// CTAs that an SM holds: of 128, 168 or 255 registers a thread
+constexpr int ctas_per_sm(bool f32, int nq) { return 5 - nq - (f32 ? 1 : 0); }
+
+// NQ: groups of eight query rows of a CTA
+template <int D, bool F32, int NQ>
+__global__ void __launch_bounds__(kThreads, ctas_per_sm(F32, NQ)) kv4_attend_kernel(const __grid_constant__ Kv4AttendParams p) {
+  constexpr int ROWS = 8 * NQ;
+  constexpr int KS = D / 16;                 // k-steps of K Q^T; tiles of 16 elements of the output
+  constexpr int NP = F32 ? 3 : 1;            // bf16 numbers that a query element, and a probability, is the sum of
   constexpr int CODES = Ring<D>::kCodes, SCALES = Ring<D>::kScales;
   extern __shared__ __align__(16) unsigned char smem[];
-  __shared__ float merge_m[kWarps][kRows], merge_l[kWarps][kRows];
+  __shared__ float merge_m[kWarps][ROWS], merge_l[kWarps][ROWS];
   pdl_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, t = lane & 3;
   const int split = blockIdx.x, unit = blockIdx.y + blockIdx.z * gridDim.y;
@@ -78,13 +93,18 @@ __global__ void __launch_bounds__(kThreads) kv4_attend_kernel(const __grid_const
   const int b = head / p.kv_heads, kvh = head - b * p.kv_heads;
   const int nq = p.new_lens ? min(max(p.new_lens[b], 0), p.n_queries) : p.n_queries;
   const int len = kv4_length(p, head, nq);
-  const int rows = nq * p.group, m0 = tile * kRows;
-  const Kv4Range range = kv4_range(p, len, nq, m0, min(m0 + kRows, rows) - 1);
+  const int rows = nq * p.group, m0 = tile * ROWS;
+  const Kv4Range range = kv4_range(p, len, nq, m0, min(m0 + ROWS, rows) - 1);
   const int chunks1 = (range.sink_end + kChunk - 1) / kChunk, chunks = m0 < rows ? chunks1 + (range.hi - range.lo + kChunk - 1) / kChunk : 0;
   const int c_begin = (int)((long long)chunks * split / p.splits), c_end = (int)((long long)chunks * (split + 1) / p.splits);
 
-  const long long row0 = first_row(p.planes, head);
   const uint32_t ring = smem_u32(smem) + warp * Ring<D>::kWarp;
+  const long long row0 = first_row(p.planes, head);
+  // the lane's place in a chunk's codes and scales, which are runs of bytes
+  const unsigned char* const kc = p.planes.k_codes + row0 * (D / 2) + lane * 16;
+  const unsigned char* const vc = p.planes.v_codes + row0 * (D / 2) + lane * 16;
+  const unsigned char* const ks_ = p.planes.k_scales + (row0 + lane) * (D / 16);
+  const unsigned char* const vs_ = p.planes.v_scales + (row0 + lane) * (D / 16);
   // Chunk c: its first stored row and the end of the rows that count
   auto chunk_at = [&](int c, int& first, int& end) {
     first = c < chunks1 ? c * kChunk : range.lo + (c - chunks1) * kChunk;
@@ -95,199 +115,209 @@ __global__ void __launch_bounds__(kThreads) kv4_attend_kernel(const __grid_const
       int first, end;
       chunk_at(c, first, end);
       const uint32_t at = ring + stage * Ring<D>::kStage;
-      constexpr int PIECES = D / 32;         // 16-byte pieces of a row's codes
+      constexpr int PIECES = CODES / 512;    // of a lane
+      const long long off = (long long)first * (D / 2), off_s = (long long)first * (D / 16);
+      if (first + kChunk <= end) {
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) {
-        const int piece = i * 32 + lane, row = piece / PIECES;
-        const bool live = first + row < end;
-        const long long src = (row0 + (live ? first + row : 0)) * (D / 2) + (piece % PIECES) * 16;
-        cp_async16(at + piece * 16, p.planes.k_codes + src, live);
-        cp_async16(at + CODES + piece * 16, p.planes.v_codes + src, live);
+        for (int i = 0; i < PIECES; ++i) {
+          cp_async<16>(at + i * 512 + lane * 16, kc + off + i * 512, 16);
+          cp_async<16>(at + CODES + i * 512 + lane * 16, vc + off + i * 512, 16);
+        }
+        cp_async<D / 16>(at + 2 * CODES + lane * (D / 16), ks_ + off_s, D / 16);
+        cp_async<D / 16>(at + 2 * CODES + SCALES + lane * (D / 16), vs_ + off_s, D / 16);
+      } else {                               // rows behind the end are filled with zeros and not read
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+          const int bytes = (i * 512 + lane * 16) / (D / 2) < end - first ? 16 : 0;
+          cp_async<16>(at + i * 512 + lane * 16, bytes ? kc + off + i * 512 : kc, bytes);
+          cp_async<16>(at + CODES + i * 512 + lane * 16, bytes ? vc + off + i * 512 : vc, bytes);
+        }
+        const int bytes = lane < end - first ? D / 16 : 0;
+        cp_async<D / 16>(at + 2 * CODES + lane * (D / 16), bytes ? ks_ + off_s : p.planes.k_scales, bytes);
+        cp_async<D / 16>(at + 2 * CODES + SCALES + lane * (D / 16), bytes ? vs_ + off_s : p.planes.v_scales, bytes);
       }
-      const bool live = first + lane < end;
-      const long long src = (row0 + (live ? first + lane : 0)) * (D / 16);
-      cp_async_small<D / 16>(at + 2 * CODES + lane * (D / 16), p.planes.k_scales + src, live);
-      cp_async_small<D / 16>(at + 2 * CODES + SCALES + lane * (D / 16), p.planes.v_scales + src, live);
     }
     cp_async_commit();
   };
 #pragma unroll
   for (int s = 0; s < kStages - 1; ++s) fetch(c_begin + warp + s * kWarps, s);
 
-  // Query fragments.  Lane t of a row holds its elements [t D/4, (t+1) D/4): code word w of them is two k-steps, of which step
-  // 2w + u takes elements 2u and 2u + 4 as its columns 2t and 2t + 1, and 2u + 1 and 2u + 5 as 2t + 8 and 2t + 9.
-  uint32_t qf[F32 ? 1 : KS][4];
-  uint4* const q_smem = reinterpret_cast<uint4*>(smem + smem_bytes<D, false>());   // fp32: [3][KS][32]
-  const int row_token[2] = {(m0 + r) / p.group, (m0 + r + 8) / p.group};
-  const int row_head[2] = {(m0 + r) % p.group, (m0 + r + 8) % p.group};
-  const bool row_live[2] = {m0 + r < rows, m0 + r + 8 < rows};
+  // Query fragments (the second operand: 16 elements x 8 query rows).  Lane t of row r holds its elements [t D/4, (t+1) D/4): code
+  // word w of them is two k-steps, of which step 2w + u takes elements 2u and 2u + 4 as its 2t and 2t + 1, and 2u + 1 and 2u + 5
+  // as 2t + 8 and 2t + 9.
+  uint2 qf[F32 ? 1 : NQ][F32 ? 1 : KS];
+  uint2* const q_smem = reinterpret_cast<uint2*>(smem + smem_bytes<D, false, NQ>());   // fp32: [3][NQ][KS][32]
 #pragma unroll
-  for (int w = 0; w < KS / 2; ++w) {
-    if (F32 && w % kWarps != warp) continue;           // the warps share the fragments
-    uint32_t part[F32 ? 3 : 1][2][4];                  // per row: pairs (0,4) (1,5) (2,6) (3,7)
+  for (int g = 0; g < NQ; ++g) {
+    const int m = m0 + 8 * g + r, token = m / p.group;
+    const bool live = m < rows;
+    const long long at = b * p.q_stride.batch + (long long)(kvh * p.group + m - token * p.group) * p.q_stride.head + token * p.q_stride.token + t * (D / 4);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const long long at = b * p.q_stride.batch + (long long)(kvh * p.group + row_head[i]) * p.q_stride.head + row_token[i] * p.q_stride.token +
-                           t * (D / 4) + w * 8;
+    for (int w = 0; w < KS / 2; ++w) {
       if constexpr (F32) {
+        if (w % kWarps != warp) continue;                // the warps share the fragments
         float x[8];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const float4 v = row_live[i] ? *reinterpret_cast<const float4*>(static_cast<const float*>(p.q) + at + 4 * e) : make_float4(0.f, 0.f, 0.f, 0.f);
+          const float4 v = live ? *reinterpret_cast<const float4*>(static_cast<const float*>(p.q) + at + w * 8 + 4 * e) : make_float4(0.f, 0.f, 0.f, 0.f);
           x[4 * e] = v.x; x[4 * e + 1] = v.y; x[4 * e + 2] = v.z; x[4 * e + 3] = v.w;
         }
 #pragma unroll
-        for (int k = 0; k < 3; ++k)
+        for (int k = 0; k < NP; ++k) {
+          uint32_t h[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const uint32_t h = pack2(x[e], x[e + 4]);
-            part[k][i][e] = h;
-            x[e] -= low(h);
-            x[e + 4] -= high(h);
+            h[e] = pack2(x[e], x[e + 4]);
+            x[e] -= low(h[e]);
+            x[e + 4] -= high(h[e]);
           }
-      } else {
-        const uint4 v = row_live[i] ? *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + at) : make_uint4(0, 0, 0, 0);
-        part[0][i][0] = __byte_perm(v.x, v.z, 0x5410);
-        part[0][i][1] = __byte_perm(v.x, v.z, 0x7632);
-        part[0][i][2] = __byte_perm(v.y, v.w, 0x5410);
-        part[0][i][3] = __byte_perm(v.y, v.w, 0x7632);
-      }
-    }
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      if constexpr (F32) {
-#pragma unroll
-        for (int k = 0; k < 3; ++k)
-          q_smem[(k * KS + 2 * w + u) * 32 + lane] = make_uint4(part[k][0][2 * u], part[k][1][2 * u], part[k][0][2 * u + 1], part[k][1][2 * u + 1]);
+          for (int u = 0; u < 2; ++u) q_smem[((k * NQ + g) * KS + 2 * w + u) * 32 + lane] = make_uint2(h[2 * u], h[2 * u + 1]);
+        }
       } else {
-        qf[2 * w + u][0] = part[0][0][2 * u];
-        qf[2 * w + u][1] = part[0][1][2 * u];
-        qf[2 * w + u][2] = part[0][0][2 * u + 1];
-        qf[2 * w + u][3] = part[0][1][2 * u + 1];
+        const uint4 v = live ? *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + at + w * 8) : make_uint4(0, 0, 0, 0);
+        qf[g][2 * w] = make_uint2(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632));
+        qf[g][2 * w + 1] = make_uint2(__byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
       }
     }
   }
   if (F32) __syncthreads();
 
-  float o[NT][4];
+  // Of group g the lane has query rows 8 g + 2 t and + 1: logits of stored rows r and r + 8 of a tile of 16, outputs of elements
+  // r D/8 + 2 i and + 1.
+  float o[NQ][KS][4], m[NQ][2], l[NQ][2];
+  int at_row[NQ][2];                           // positions
 #pragma unroll
-  for (int j = 0; j < NT; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
-  float m[2] = {kNoLogit, kNoLogit}, l[2] = {0.f, 0.f};
+  for (int g = 0; g < NQ; ++g) {
+#pragma unroll
+    for (int i = 0; i < KS; ++i) o[g][i][0] = o[g][i][1] = o[g][i][2] = o[g][i][3] = 0.f;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      m[g][e] = kNoLogit;
+      l[g][e] = 0.f;
+      at_row[g][e] = len - nq + (m0 + 8 * g + 2 * t + e) / p.group;
+    }
+  }
   const float c = p.scale_log2;
-  const int at_row[2] = {len - nq + row_token[0], len - nq + row_token[1]};
 
   int stage = 0;
+#pragma unroll 1
   for (int ch = c_begin + warp; ch < c_end; ch += kWarps) {
     cp_async_wait<kStages - 2>();
     __syncwarp();
     int first, end;
     chunk_at(ch, first, end);
     const unsigned char* at = smem + warp * Ring<D>::kWarp + stage * Ring<D>::kStage;
-    // ---- logits: four tiles of eight stored rows
-    float s[4][4];
+    // ---- logits: two tiles of 16 stored rows
+    float s[NQ][2][4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
-      const int row = 8 * j + r;
-      uint32_t w[KS / 2];
-      if constexpr (D == 128) {
-        const uint4 v = *reinterpret_cast<const uint4*>(at + row * 64 + t * 16);
-        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-      } else {
-        const uint2 v = *reinterpret_cast<const uint2*>(at + row * 32 + t * 8);
-        w[0] = v.x; w[1] = v.y;
+    for (int T = 0; T < 2; ++T) {
+#pragma unroll
+      for (int g = 0; g < NQ; ++g) s[g][T][0] = s[g][T][1] = s[g][T][2] = s[g][T][3] = 0.f;
+      uint32_t w[2][KS / 2];
+      Scale2 sc[2][D / 64];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {            // stored rows r and r + 8 of the tile
+        const int row = 16 * T + 8 * i + r;
+        if constexpr (D == 128) {
+          const uint4 v = *reinterpret_cast<const uint4*>(at + row * 64 + t * 16);
+          w[i][0] = v.x; w[i][1] = v.y; w[i][2] = v.z; w[i][3] = v.w;
+          const uint32_t bytes = *reinterpret_cast<const uint16_t*>(at + 2 * CODES + row * 8 + t * 2);
+          sc[i][0] = scale2(__byte_perm(bytes, 0, 0x4040));
+          sc[i][1] = scale2(__byte_perm(bytes, 0, 0x4141));
+        } else {
+          const uint2 v = *reinterpret_cast<const uint2*>(at + row * 32 + t * 8);
+          w[i][0] = v.x; w[i][1] = v.y;
+          sc[i][0] = scale2(at[2 * CODES + row * 4 + t] * 0x10001u);
+        }
       }
 #pragma unroll
-      for (int blk = 0; blk < D / 64; ++blk) {
-        const uint32_t byte = at[2 * CODES + row * (D / 16) + t * (D / 64) + blk];
-        const Scale2 sc = scale2(byte | byte << 16);
+      for (int x = 0; x < KS / 2; ++x)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint32_t word = w[2 * blk + i];
+        for (int u = 0; u < 2; ++u) {
+          const Scale2 &s0 = sc[0][x / 2], &s1 = sc[1][x / 2];
+          const uint32_t a0 = values2(w[0][x], 8 * u, s0), a1 = values2(w[1][x], 8 * u, s1);
+          const uint32_t a2 = values2(w[0][x], 8 * u + 4, s0), a3 = values2(w[1][x], 8 * u + 4, s1);
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const uint32_t b0 = values2(word, 8 * u, sc), b1 = values2(word, 8 * u + 4, sc);
-            const int ks = 2 * (2 * blk + i) + u;
+          for (int g = 0; g < NQ; ++g) {
             if constexpr (F32) {
 #pragma unroll
-              for (int k = 2; k >= 0; --k) {
-                const uint4 a = q_smem[(k * KS + ks) * 32 + lane];
-                mma16816(s[j], reinterpret_cast<const uint32_t*>(&a), b0, b1);
+              for (int k = NP - 1; k >= 0; --k) {
+                const uint2 q = q_smem[((k * NQ + g) * KS + 2 * x + u) * 32 + lane];
+                mma(s[g][T], a0, a1, a2, a3, q.x, q.y);
               }
             } else {
-              mma16816(s[j], qf[ks], b0, b1);
+              mma(s[g][T], a0, a1, a2, a3, qf[g][2 * x + u].x, qf[g][2 * x + u].y);
             }
           }
         }
-      }
     }
-    // ---- softmax.  Stored rows of this lane: first + 8 j + 2 t + (0, 1)
+    // ---- softmax
     if (first + kChunk > end || !kv4_all_see(p, range, first)) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int g = 0; g < NQ; ++g)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int row = first + 8 * j + 2 * t + (e & 1);
-          if (row >= end || !kv4_sees(p, at_row[e >> 1], row)) s[j][e] = -INFINITY;
-        }
-    }
-    float top[2];
+        for (int T = 0; T < 2; ++T)
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      top[i] = fmaxf(fmaxf(fmaxf(s[0][2 * i], s[0][2 * i + 1]), fmaxf(s[1][2 * i], s[1][2 * i + 1])),
-                     fmaxf(fmaxf(s[2][2 * i], s[2][2 * i + 1]), fmaxf(s[3][2 * i], s[3][2 * i + 1])));
-    }
-    if (__any_sync(0xffffffffu, (top[0] - m[0]) * c > kRaise || (top[1] - m[1]) * c > kRaise)) {
-      float f[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        float mx = fmaxf(m[i], top[i]);
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-        f[i] = ex2((m[i] - mx) * c);
-        m[i] = mx;
-        l[i] *= f[i];
-      }
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        o[j][0] *= f[0]; o[j][1] *= f[0];
-        o[j][2] *= f[1]; o[j][3] *= f[1];
-      }
-    }
-    // (a row that has seen nothing yet has a reference of -3.4e38, whose product may overflow)
-    const float nmc[2] = {m[0] == kNoLogit ? 0.f : -m[0] * c, m[1] == kNoLogit ? 0.f : -m[1] * c};
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s[j][e] = ex2(fmaf(s[j][e], c, nmc[e >> 1]));
-    // ---- values: two steps of sixteen stored rows; the sums are of the probabilities as the products see them
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      uint32_t pf[F32 ? 3 : 1][4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float x = s[2 * k + (i >> 1)][2 * (i & 1)], y = s[2 * k + (i >> 1)][2 * (i & 1) + 1];
-        if constexpr (F32) {
-          l[i & 1] += x + y;
-#pragma unroll
-          for (int q = 0; q < 3; ++q) {
-            const uint32_t h = pack2(x, y);
-            pf[q][i] = h;
-            x -= low(h);
-            y -= high(h);
+          for (int e = 0; e < 4; ++e) {
+            const int row = first + 16 * T + 8 * (e >> 1) + r;
+            if (row >= end || !kv4_sees(p, at_row[g][e & 1], row)) s[g][T][e] = -INFINITY;
           }
-        } else {
-          pf[0][i] = pack2(x, y);
-          l[i & 1] += low(pf[0][i]) + high(pf[0][i]);
-        }
+    }
+    float top[NQ][2];
+    bool raise = false;
+#pragma unroll
+    for (int g = 0; g < NQ; ++g)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        top[g][e] = fmaxf(fmaxf(s[g][0][e], s[g][0][2 + e]), fmaxf(s[g][1][e], s[g][1][2 + e]));
+        raise |= (top[g][e] - m[g][e]) * c > kRaise;
       }
+    if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+      for (int g = 0; g < NQ; ++g)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float mx = fmaxf(m[g][e], top[g][e]);
+#pragma unroll
+          for (int x = 4; x < 32; x *= 2) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
+          const float f = ex2((m[g][e] - mx) * c);
+          m[g][e] = mx;
+          l[g][e] *= f;
+#pragma unroll
+          for (int i = 0; i < KS; ++i) { o[g][i][e] *= f; o[g][i][2 + e] *= f; }
+        }
+    }
+    // the probabilities as the second operand of the products with the values: 16 stored rows x 8 query rows
+    uint32_t pf[NP][NQ][2][2];
+#pragma unroll
+    for (int g = 0; g < NQ; ++g) {
+      // (a row that has seen nothing yet has a reference of -3.4e38, whose product may overflow)
+      const float n0 = m[g][0] == kNoLogit ? 0.f : -m[g][0] * c, n1 = m[g][1] == kNoLogit ? 0.f : -m[g][1] * c;
+#pragma unroll
+      for (int T = 0; T < 2; ++T)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float x = ex2(fmaf(s[g][T][2 * i], c, n0)), y = ex2(fmaf(s[g][T][2 * i + 1], c, n1));
+          if constexpr (F32) { l[g][0] += x; l[g][1] += y; }
+#pragma unroll
+          for (int k = 0; k < NP; ++k) {
+            const uint32_t h = pack2(x, y);
+            if constexpr (F32) { x -= low(h); y -= high(h); }
+            else add_bf162(l[g][0], l[g][1], h);       // the sums are of what the products see
+            pf[k][g][T][i] = transposed(h);
+          }
+        }
+    }
+    // ---- values
+#pragma unroll
+    for (int T = 0; T < 2; ++T) {
       const unsigned char* codes = at + CODES + r * (D / 16);
       const unsigned char* scales = at + 2 * CODES + SCALES + (r * (D / 8)) / kBlock;
-      uint32_t w[4][D / 64];
-      uint32_t byte[4];
+      uint32_t w[4][D / 64], byte[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {          // rows 2t, 2t + 1, 2t + 8, 2t + 9
-        const int row = 16 * k + 2 * t + (i & 1) + 8 * (i >> 1);
+      for (int i = 0; i < 4; ++i) {          // stored rows 2t, 2t + 1, 2t + 8, 2t + 9
+        const int row = 16 * T + 2 * t + (i & 1) + 8 * (i >> 1);
         if constexpr (D == 128) {
           const uint2 v = *reinterpret_cast<const uint2*>(codes + row * 64);
           w[i][0] = v.x; w[i][1] = v.y;
@@ -304,10 +334,12 @@ __global__ void __launch_bounds__(kThreads) kv4_attend_kernel(const __grid_const
           const uint32_t sel = half ? 0x7632 : 0x5410;
           const uint32_t w0 = __byte_perm(w[0][x], w[1][x], sel), w1 = __byte_perm(w[2][x], w[3][x], sel);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t b0 = values2(w0, 4 * i, s0), b1 = values2(w1, 4 * i, s1);
+          for (int i = 0; i < 2; ++i) {      // elements 8 x + 4 half + 2 i and + 1 of the lane's
+            const uint32_t a0 = values2(w0, 8 * i, s0), a1 = values2(w0, 8 * i + 4, s0), a2 = values2(w1, 8 * i, s1), a3 = values2(w1, 8 * i + 4, s1);
 #pragma unroll
-            for (int q = F32 ? 2 : 0; q >= 0; --q) mma16816(o[8 * x + 4 * half + i], pf[q], b0, b1);
+            for (int g = 0; g < NQ; ++g)
+#pragma unroll
+              for (int k = NP - 1; k >= 0; --k) mma(o[g][4 * x + 2 * half + i], a0, a1, a2, a3, pf[k][g][T][0], pf[k][g][T][1]);
           }
         }
     }
@@ -319,49 +351,50 @@ __global__ void __launch_bounds__(kThreads) kv4_attend_kernel(const __grid_const
 
   // ---- the warps' shares
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
-    l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-    if (t == 0) merge_m[warp][r + 8 * i] = m[i];
-  }
+  for (int g = 0; g < NQ; ++g)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+      for (int x = 4; x < 32; x *= 2) l[g][e] += __shfl_xor_sync(0xffffffffu, l[g][e], x);
+      if (r == 0) merge_m[warp][8 * g + 2 * t + e] = m[g][e];
+    }
   __syncthreads();                           // (and every warp is done with its ring)
-  float f[2];
+  float* const mine = reinterpret_cast<float*>(smem) + warp * ROWS * D;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    float mx = merge_m[0][r + 8 * i];
+  for (int g = 0; g < NQ; ++g)
 #pragma unroll
-    for (int w = 1; w < kWarps; ++w) mx = fmaxf(mx, merge_m[w][r + 8 * i]);
-    f[i] = ex2((m[i] - mx) * c);
-    if (t == 0) merge_l[warp][r + 8 * i] = l[i] * f[i];
-  }
-  float* const mine = reinterpret_cast<float*>(smem) + warp * kRows * D;
+    for (int e = 0; e < 2; ++e) {
+      const int row = 8 * g + 2 * t + e;
+      float mx = merge_m[0][row];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+      for (int w = 1; w < kWarps; ++w) mx = fmaxf(mx, merge_m[w][row]);
+      const float f = ex2((m[g][e] - mx) * c);
+      if (r == 0) merge_l[warp][row] = l[g][e] * f;
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
-#pragma unroll
-      for (int j = 0; j < NT; j += 4)
-        *reinterpret_cast<float4*>(mine + (r + 8 * i) * D + (2 * t + e) * NT + j) =
-            make_float4(o[j][2 * i + e] * f[i], o[j + 1][2 * i + e] * f[i], o[j + 2][2 * i + e] * f[i], o[j + 3][2 * i + e] * f[i]);
+      for (int i = 0; i < KS; i += 2)
+        *reinterpret_cast<float4*>(mine + row * D + r * (D / 8) + 2 * i) =
+            make_float4(o[g][i][e] * f, o[g][i][2 + e] * f, o[g][i + 1][e] * f, o[g][i + 1][2 + e] * f);
+    }
   __syncthreads();
-  for (int x = threadIdx.x; x < kRows * D / 4; x += kThreads) {
+#pragma unroll 1
+  for (int x = threadIdx.x; x < ROWS * D / 4; x += kThreads) {
     const int row = x / (D / 4), d = (x - row * (D / 4)) * 4;
+    if (m0 + row >= rows) break;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
     float total = 0.f, mx = kNoLogit;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
-      const float4 v = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(smem) + (w * kRows + row) * D + d);
+      const float4 v = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(smem) + (w * ROWS + row) * D + d);
       sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
       total += merge_l[w][row];
       mx = fmaxf(mx, merge_m[w][row]);
     }
-    if (m0 + row >= rows) continue;
     if (p.splits > 1) {
-      float* part = p.partial + ((long long)unit * p.splits + split) * (kRows * (D + 2));
+      float* part = p.partial + ((long long)unit * p.splits + split) * (ROWS * (D + 2));
       *reinterpret_cast<float4*>(part + row * D + d) = sum;
       if (d == 0) {
-        part[kRows * D + 2 * row] = mx;
-        part[kRows * D + 2 * row + 1] = total;
+        part[ROWS * D + 2 * row] = mx;
+        part[ROWS * D + 2 * row + 1] = total;
       }
     } else {
       kv4_store<F32>(p, b, kvh, m0 + row, d, sum, total);
@@ -398,16 +431,19 @@ __global__ void __launch_bounds__(256) kv4_combine_kernel(const __grid_constant_
   kv4_store<F32>(p, b, kvh, m, d, sum, total);
 }
 
+template <int D, bool F32, int NQ>
+int launch_few(const Kv4AttendParams& p, cudaStream_t st) {
+  constexpr size_t smem = smem_bytes<D, F32, NQ>();
+  if (!allow_dynamic_smem(kv4_attend_kernel<D, F32, NQ>, smem)) return -1;
+  const int y = std::min(p.units, 32768);
+  launch_k(kv4_attend_kernel<D, F32, NQ>, dim3(p.splits, y, (p.units + y - 1) / y), dim3(kThreads), smem, st, p);
+  return 1;
+}
+
 template <int D, bool F32>
 int launch_attend(const Kv4AttendParams& p, cudaStream_t st) {
-  if (p.tile_rows == kRows) {
-    constexpr size_t smem = smem_bytes<D, F32>();
-    if (!allow_dynamic_smem(kv4_attend_kernel<D, F32>, smem)) return -1;
-    const int y = std::min(p.units, 32768);
-    launch_k(kv4_attend_kernel<D, F32>, dim3(p.splits, y, (p.units + y - 1) / y), dim3(kThreads), smem, st, p);
-  } else if (launch_kv4_attend_tc(p, D, st) < 0) {
-    return -1;
-  }
+  const int r = p.tile_rows == 8 ? launch_few<D, F32, 1>(p, st) : p.tile_rows == 16 ? launch_few<D, F32, 2>(p, st) : launch_kv4_attend_tc(p, D, st);
+  if (r < 0) return -1;
   if (p.splits > 1) {
     constexpr int PER = 256 / (D / 4);
     launch_k(kv4_combine_kernel<D, F32>, dim3((unsigned)(((long long)p.units * p.tile_rows + PER - 1) / PER)), dim3(256), 0, st, p);
@@ -446,7 +482,7 @@ hack_status_t plan(const hack_kv4_t* kv, const hack_kv4_attend_t* a, Kv4AttendPa
   p.appended = a->appended != 0;
   const int heads = kv->batch * kv->n_kv_heads, rows = a->n_queries * p.group;
   const bool tc = a->dtype == HACK_BF16 && rows >= kTcRows;
-  p.tile_rows = tc ? 128 : kRows;
+  p.tile_rows = tc ? 128 : rows <= 8 ? 8 : 16;
   p.tiles = (rows + p.tile_rows - 1) / p.tile_rows;
   const long long units = (long long)heads * p.tiles;
   if (units > 0x3fffffffll) { set_error("more query rows than a launch has places for"); return HACK_ERR_UNSUPPORTED; }
@@ -460,8 +496,16 @@ hack_status_t plan(const hack_kv4_t* kv, const hack_kv4_attend_t* a, Kv4AttendPa
     const long long ctas = (long long)heads * ((p.tiles + p.tiles_per_cta - 1) / p.tiles_per_cta);
     p.splits = (int)std::max<long long>(1, std::min<long long>((walked + 127) / 128 / 4, sms / ctas));
   } else {
-    const long long turns = (walked + kChunk * kWarps - 1) / (kChunk * kWarps);
-    p.splits = (int)std::max<long long>(1, std::min<long long>(turns / 2, 4ll * sms / units));
+    // CTAs that share a unit's rows: as few turns one behind the other as can be, counting what a CTA, a second launch and a
+    // share in it cost in turns
+    const long long turns = std::max<long long>(1, (walked + kChunk * kWarps - 1) / (kChunk * kWarps));
+    const long long places = (long long)sms * ctas_per_sm(a->dtype == HACK_F32, p.tile_rows / 8);
+    double best = 0;
+    p.splits = 1;
+    for (int n = 1; n <= 64 && n <= turns; ++n) {
+      const double cost = (double)((units * n + places - 1) / places) * ((double)((turns + n - 1) / n) + 3.0) + (n > 1 ? 3.0 + 0.1 * n : 0.0);
+      if (n == 1 || cost < best) { best = cost; p.splits = n; }
+    }
   }
   p.wait_polls = a->wait_polls > 0 ? (uint32_t)a->wait_polls : kWaitPolls;
   workspace = p.splits > 1 ? (size_t)p.units * p.splits * p.tile_rows * (kv->head_dim + 2) * 4 : 0;

@@ -10,7 +10,7 @@ struct Kv4AttendParams {
   int kv_heads, group;              // group: query heads of a stored head
   int n_queries, max_len;
   int causal, window, n_sink, appended;
-  int tile_rows;                    // query rows of a tile: 16, or 128 on the tensor cores
+  int tile_rows;                    // query rows of a tile: 8 or 16, or 128 on the tensor cores
   int tiles, units, splits;         // tiles of query rows of a stored head, all of them, CTAs that share the rows of one
   int tiles_per_cta;                // tensor cores: 1 or 2
   int out_sectors;                  // rows of the output start on 32-byte boundaries

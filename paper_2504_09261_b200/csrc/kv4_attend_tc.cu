@@ -57,11 +57,6 @@ __device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, Bars* b
   return true;
 }
 
-// x += the low, y += the high bf16 number of w
-__device__ __forceinline__ void add_bf162(float& x, float& y, uint32_t w) {
-  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tadd.rn.f32.bf16 %0, l, %0;\n\tadd.rn.f32.bf16 %1, h, %1;\n\t}" : "+f"(x), "+f"(y) : "r"(w));
-}
-
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid_constant__ Kv4AttendParams p) {
   constexpr uint32_t SUB_BYTES = kBN * 128, TILE_BYTES = D / 64 * SUB_BYTES;      // tiles of 64 columns: 128 rows x 128 bytes
