@@ -31,6 +31,7 @@ using ptx::ex2;
 using ptx::smem_u32;
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
+constexpr int kCombineThreads = 256, kMaxSplits = 64;
 constexpr int kChunk = 32;                   // stored rows of a turn of a warp
 constexpr int kStages = 3;
 constexpr float kRaise = 16.f;               // log2 by which a logit may exceed the reference maximum
@@ -402,14 +403,15 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(F32, NQ)) kv4_attend_ker
   }
 }
 
-// Partial results of the splits added up: D / 4 threads for a query row.
+// Partial results of the splits (at most 64) added up: a CTA for a query row, its groups of D / 4 threads share the splits.  (One
+// group for all of them, one after the other, took 0.3 us a split.)
 template <int D, bool F32>
-__global__ void __launch_bounds__(256) kv4_combine_kernel(const __grid_constant__ Kv4AttendParams p) {
+__global__ void __launch_bounds__(kCombineThreads) kv4_combine_kernel(const __grid_constant__ Kv4AttendParams p) {
+  constexpr int LANES = D / 4, GROUPS = kCombineThreads / LANES;
+  __shared__ float weight[kMaxSplits];
+  __shared__ float4 sums[GROUPS][LANES];
   pdl_wait();
-  constexpr int LANES = D / 4, PER = 256 / LANES;
-  const long long index = (long long)blockIdx.x * PER + threadIdx.x / LANES;
-  const int unit = (int)(index / p.tile_rows), row = (int)(index - (long long)unit * p.tile_rows), d = (threadIdx.x % LANES) * 4;
-  if (unit >= p.units) return;
+  const int unit = blockIdx.x / p.tile_rows, row = blockIdx.x - unit * p.tile_rows;
   const int head = unit / p.tiles, tile = unit - head * p.tiles;
   const int b = head / p.kv_heads, kvh = head - b * p.kv_heads;
   const int nq = p.new_lens ? min(max(p.new_lens[b], 0), p.n_queries) : p.n_queries;
@@ -417,17 +419,51 @@ __global__ void __launch_bounds__(256) kv4_combine_kernel(const __grid_constant_
   if (m >= nq * p.group) return;
   const long long step = (long long)p.tile_rows * (D + 2);
   const float* part = p.partial + (long long)unit * p.splits * step;
-  const float* stats = part + (long long)p.tile_rows * D + 2 * row;
-  float mx = kNoLogit;
-  for (int s = 0; s < p.splits; ++s) mx = fmaxf(mx, stats[s * step]);
-  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+  const int lane = threadIdx.x & 31, group = threadIdx.x / LANES, d = (threadIdx.x % LANES) * 4;
+  // the first outputs are on their way while the weights are formed
+  constexpr int AHEAD = 4;
+  float4 v[AHEAD];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+    if (group + i * GROUPS < p.splits) v[i] = *reinterpret_cast<const float4*>(part + (group + i * GROUPS) * step + (long long)row * D + d);
   float total = 0.f;
-  for (int s = 0; s < p.splits; ++s) {
-    const float f = ex2((stats[s * step] - mx) * p.scale_log2);
-    const float4 v = *reinterpret_cast<const float4*>(part + s * step + (long long)row * D + d);
-    total += f * stats[s * step + 1];
-    sum.x = fmaf(f, v.x, sum.x); sum.y = fmaf(f, v.y, sum.y); sum.z = fmaf(f, v.z, sum.z); sum.w = fmaf(f, v.w, sum.w);
+  {
+    // every warp for itself: reference maximum and sum of splits lane and lane + 32
+    const float* stats = part + (long long)p.tile_rows * D + 2 * row;
+    float2 x[2];
+    float mx = kNoLogit;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int s = lane + 32 * i;
+      x[i] = s < p.splits ? *reinterpret_cast<const float2*>(stats + s * step) : make_float2(kNoLogit, 0.f);
+      mx = fmaxf(mx, x[i].x);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float f = ex2((x[i].x - mx) * p.scale_log2);
+      total += f * x[i].y;
+      if (threadIdx.x < 32) weight[lane + 32 * i] = f;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
   }
+  __syncthreads();
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](const float4& x, float f) {
+    sum.x = fmaf(f, x.x, sum.x); sum.y = fmaf(f, x.y, sum.y); sum.z = fmaf(f, x.z, sum.z); sum.w = fmaf(f, x.w, sum.w);
+  };
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+    if (group + i * GROUPS < p.splits) add(v[i], weight[group + i * GROUPS]);
+  for (int s = group + AHEAD * GROUPS; s < p.splits; s += GROUPS)
+    add(*reinterpret_cast<const float4*>(part + s * step + (long long)row * D + d), weight[s]);
+  sums[group][threadIdx.x % LANES] = sum;
+  __syncthreads();
+  if (group > 0) return;
+#pragma unroll
+  for (int g = 1; g < GROUPS; ++g) add(sums[g][threadIdx.x], 1.f);
   kv4_store<F32>(p, b, kvh, m, d, sum, total);
 }
 
@@ -445,8 +481,7 @@ int launch_attend(const Kv4AttendParams& p, cudaStream_t st) {
   const int r = p.tile_rows == 8 ? launch_few<D, F32, 1>(p, st) : p.tile_rows == 16 ? launch_few<D, F32, 2>(p, st) : launch_kv4_attend_tc(p, D, st);
   if (r < 0) return -1;
   if (p.splits > 1) {
-    constexpr int PER = 256 / (D / 4);
-    launch_k(kv4_combine_kernel<D, F32>, dim3((unsigned)(((long long)p.units * p.tile_rows + PER - 1) / PER)), dim3(256), 0, st, p);
+    launch_k(kv4_combine_kernel<D, F32>, dim3((unsigned)p.units * p.tile_rows), dim3(kCombineThreads), 0, st, p);
   }
   return launched(1);
 }
@@ -485,7 +520,7 @@ hack_status_t plan(const hack_kv4_t* kv, const hack_kv4_attend_t* a, Kv4AttendPa
   p.tile_rows = tc ? 128 : rows <= 8 ? 8 : 16;
   p.tiles = (rows + p.tile_rows - 1) / p.tile_rows;
   const long long units = (long long)heads * p.tiles;
-  if (units > 0x3fffffffll) { set_error("more query rows than a launch has places for"); return HACK_ERR_UNSUPPORTED; }
+  if (units * p.tile_rows > 0x3fffffffll) { set_error("more query rows than a launch has places for"); return HACK_ERR_UNSUPPORTED; }
   p.units = (int)units;
   // rows that a tile of queries walks at most
   long long walked = p.max_len;
@@ -494,7 +529,7 @@ hack_status_t plan(const hack_kv4_t* kv, const hack_kv4_attend_t* a, Kv4AttendPa
   if (tc) {
     p.tiles_per_cta = units <= sms ? 1 : 2;
     const long long ctas = (long long)heads * ((p.tiles + p.tiles_per_cta - 1) / p.tiles_per_cta);
-    p.splits = (int)std::max<long long>(1, std::min<long long>((walked + 127) / 128 / 4, sms / ctas));
+    p.splits = (int)std::max<long long>(1, std::min<long long>({(walked + 127) / 128 / 4, sms / ctas, kMaxSplits}));
   } else {
     // CTAs that share a unit's rows: as few turns one behind the other as can be, counting what a CTA, a second launch and a
     // share in it cost in turns
@@ -502,7 +537,7 @@ hack_status_t plan(const hack_kv4_t* kv, const hack_kv4_attend_t* a, Kv4AttendPa
     const long long places = (long long)sms * ctas_per_sm(a->dtype == HACK_F32, p.tile_rows / 8);
     double best = 0;
     p.splits = 1;
-    for (int n = 1; n <= 64 && n <= turns; ++n) {
+    for (int n = 1; n <= kMaxSplits && n <= turns; ++n) {
       const double cost = (double)((units * n + places - 1) / places) * ((double)((turns + n - 1) / n) + 3.0) + (n > 1 ? 3.0 + 0.1 * n : 0.0);
       if (n == 1 || cost < best) { best = cost; p.splits = n; }
     }
