@@ -1,12 +1,16 @@
 // Rows into a cache of 4 bits (format: hack.h) and back.
 //
 // A thread owns a block of 16 elements of K and the same block of V: 32 (bf16) or 64 (fp32) bytes in, eight bytes of codes and
-// one of scale out, so that a warp reads and writes consecutive bytes, and nothing is exchanged.  Bound:
-// bytes; the rounding to the nearest code, exact in spite of an inexact reciprocal, stays under them.
+// one of scale out, so that a warp reads and writes consecutive bytes, and nothing is exchanged.  Bound: bytes, if the
+// arithmetic stays under them: about a dozen instructions an element in (largest of a block on the bits; one FMA that
+// rounds into the low bits of a number, and one that shows whether it fell on the wrong side, as the reciprocal is inexact),
+// two an element out (codes to bf16 as in the attention; a conversion of integers an element took 30 us of the special-function
+// unit's time where the bytes take 26).
 #include <string>
 
 #include "entry_checks.h"
 #include "kv4.cuh"
+#include "tc_ptx.cuh"
 
 namespace hack {
 namespace {
@@ -17,8 +21,9 @@ constexpr int kThreads = 256;
 
 struct RowsParams {
   Planes planes;
-  int n_tokens, blocks;               // rows of a head at most; blocks per row
+  int n_tokens;                       // rows of a head at most
   int kv_heads;
+  int whole;                          // the blocks of k and v start on 32-byte boundaries
   long long threads;                  // heads * n_tokens * blocks
   hack_strides_t ks, vs;
   const void *k, *v;                  // append; the outputs of a read
@@ -30,107 +35,126 @@ struct RowsParams {
   int src_len[2];                     // rows of a head of each type
 };
 
-template <typename T> struct Sixteen;           // 16 elements of a row
-template <> struct Sixteen<float> {
-  uint4 u[4];
-  __device__ __forceinline__ void load(const void* p) {
+// 16 elements of a row as words; `whole`: they start on a 32-byte boundary.
+__device__ __forceinline__ void load_32b(const void* p, uint32_t* w, bool whole) {
+  if (whole) {
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p) : "memory");
+  } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) u[i] = static_cast<const uint4*>(p)[i];
-  }
-  __device__ __forceinline__ void values(float* x) const {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[4 * i] = __uint_as_float(u[i].x); x[4 * i + 1] = __uint_as_float(u[i].y);
-      x[4 * i + 2] = __uint_as_float(u[i].z); x[4 * i + 3] = __uint_as_float(u[i].w);
+    for (int i = 0; i < 2; ++i) {
+      const uint4 u = static_cast<const uint4*>(p)[i];
+      w[4 * i] = u.x; w[4 * i + 1] = u.y; w[4 * i + 2] = u.z; w[4 * i + 3] = u.w;
     }
   }
-  static __device__ __forceinline__ void store(void* p, const float* x) {
+}
+template <typename T> struct Sixteen;
+template <> struct Sixteen<float> {
+  uint32_t w[16];
+  __device__ __forceinline__ void load(const void* p, bool whole) {
+    load_32b(p, w, whole);
+    load_32b(static_cast<const float*>(p) + 8, w + 8, whole);
+  }
+  __device__ __forceinline__ float at(int i) const { return __uint_as_float(w[i]); }
+  // bits of the largest magnitude; any NaN is above infinity
+  __device__ __forceinline__ uint32_t top() const {
+    uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) static_cast<float4*>(p)[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+    for (int i = 0; i < 16; ++i) m = max(m, w[i] & 0x7fffffffu);
+    return m;
+  }
+  __device__ __forceinline__ void no_nans() {
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if ((w[i] & 0x7fffffffu) > 0x7f800000u) w[i] = 0;
   }
 };
 template <> struct Sixteen<__nv_bfloat16> {
-  uint4 u[2];
-  __device__ __forceinline__ void load(const void* p) {
+  uint32_t w[8];
+  __device__ __forceinline__ void load(const void* p, bool whole) { load_32b(p, w, whole); }
+  __device__ __forceinline__ float at(int i) const { return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16); }
+  __device__ __forceinline__ uint32_t top() const {
+    uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) u[i] = static_cast<const uint4*>(p)[i];
+    for (int i = 0; i < 8; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
+    return max(m & 0xffff0000u, m << 16);
   }
-  __device__ __forceinline__ void values(float* x) const {
+  __device__ __forceinline__ void no_nans() {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint32_t w[4] = {u[i].x, u[i].y, u[i].z, u[i].w};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        x[8 * i + 2 * j] = __uint_as_float(w[j] << 16);
-        x[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-      }
-    }
-  }
-  static __device__ __forceinline__ void store(void* p, const float* x) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      uint32_t w[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(x[8 * i + 2 * j], x[8 * i + 2 * j + 1]);
-        w[j] = *reinterpret_cast<const uint32_t*>(&h);
-      }
-      static_cast<uint4*>(p)[i] = make_uint4(w[0], w[1], w[2], w[3]);
+    for (int i = 0; i < 8; ++i) {
+      if ((w[i] & 0x7fffu) > 0x7f80u) w[i] &= 0xffff0000u;
+      if ((w[i] & 0x7fff0000u) > 0x7f800000u) w[i] &= 0xffffu;
     }
   }
 };
 
 // Scale byte and codes of a block.
-__device__ __forceinline__ uint2 quantise(float* x, uint32_t& byte) {
-  float top = 0.f;
-#pragma unroll
-  for (int i = 0; i < kBlock; ++i) {
-    x[i] = x[i] == x[i] ? x[i] : 0.f;
-    top = fmaxf(top, fabsf(x[i]));
+template <typename T> __device__ __forceinline__ uint2 quantise(Sixteen<T>& x, uint32_t& byte) {
+  uint32_t top_bits = x.top();
+  if (top_bits > 0x7f800000u) {
+    x.no_nans();
+    top_bits = x.top();
   }
+  const float top = __uint_as_float(top_bits);
   // The smallest s with 7 s >= top: the rounded quotient, to three mantissa bits upwards, is it or a neighbour (7 s is exact)
   const uint32_t up = (__float_as_uint(fminf(top * (1.f / 7.f), 3840.f)) + 0xfffffu) >> 20;
   int e = min(max((int)up - (int)((127 - 20) << 3), 0), 255);
   if (e < 255 && 7.f * scale_value(e) < top) ++e;
   if (e > 0 && 7.f * scale_value(e - 1) >= top) --e;
   byte = e;
-  const float s = scale_value(e), inv = 1.f / s, half = 0.5f * s;
+  const float s = scale_value(e), inv = 1.f / s, most = 7.f * s;
+  const int half = __float_as_int(0.5f * s);
+  const bool beyond = top > most;              // the largest scale of all: what lies beyond seven of it is limited
+  // x inv + kMagic has c + 8 in its low bits.  The inexact inv may put it on the wrong side of the middle between two
+  // codes, or off it: what is left of x beside the code, which is exact, tells.
+  constexpr float kMagic = 12582912.f + 8.f;
   uint32_t code[2] = {0, 0};
 #pragma unroll
   for (int i = 0; i < kBlock; ++i) {
-    // x * inv may fall on the wrong side of the middle between two codes, or on it; what is left of x beside the code is exact
-    float t = rintf(fminf(fmaxf(x[i] * inv, -7.f), 7.f));
-    const float left = fmaf(-t, s, x[i]);
-    const bool odd = (int)t & 1;
-    if (left > half || (odd && left == half)) t += 1.f;
-    if (left < -half || (odd && left == -half)) t -= 1.f;
-    t = fminf(fmaxf(t, -7.f), 7.f);
-    code[i >> 3] |= (uint32_t)((int)t + 8) << (4 * (i & 7));
+    float v = x.at(i);
+    if (beyond) v = fminf(fmaxf(v, -most), most);
+    const float r = fmaf(v, inv, kMagic);
+    int n = __float_as_int(r);
+    const float left = fmaf(kMagic - r, s, v);
+    // on the middle, an odd code gives way: the float below one half of s
+    if (fabsf(left) > __int_as_float(half - (n & 1))) n += (__float_as_int(left) >> 31) | 1;
+    code[i >> 3] += (uint32_t)n << (4 * (i & 7));
   }
-  return make_uint2(code[0], code[1]);
+  // (the bits of kMagic without its 8, once for each of the eight codes)
+  constexpr uint32_t kBase = 0x4b400000u;
+  uint32_t extra = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) extra += kBase << (4 * i);
+  return make_uint2(code[0] - extra, code[1] - extra);
 }
 
 // Head, token and block of a thread; false past the end.
-__device__ __forceinline__ bool place(const RowsParams& p, int& head, int& token, int& block) {
+template <int BLOCKS> __device__ __forceinline__ bool place(const RowsParams& p, int& head, int& token, int& block) {
   const long long at = (long long)blockIdx.x * kThreads + threadIdx.x;
   if (at >= p.threads) return false;
-  block = (int)(at % p.blocks);
-  const long long row = at / p.blocks;
-  head = (int)(row / p.n_tokens);
-  token = (int)(row - (long long)head * p.n_tokens);
+  block = (int)(at % BLOCKS);
+  if (p.threads <= 0x7fffffffll) {
+    const uint32_t row = (uint32_t)at / BLOCKS;
+    head = row / (uint32_t)p.n_tokens;
+    token = row - (uint32_t)head * (uint32_t)p.n_tokens;
+  } else {
+    const long long row = at / BLOCKS;
+    head = (int)(row / p.n_tokens);
+    token = (int)(row - (long long)head * p.n_tokens);
+  }
   return true;
 }
 
-template <typename T>
+template <typename T, int BLOCKS>
 __global__ void __launch_bounds__(kThreads) kv4_append_kernel(const __grid_constant__ RowsParams p) {
   pdl_wait();
   int head, token, block;
-  if (!place(p, head, token, block)) return;
+  if (!place<BLOCKS>(p, head, token, block)) return;
   const int b = head / p.kv_heads, h = head - b * p.kv_heads;
   const T *k = static_cast<const T*>(p.k) + block * kBlock, *v = static_cast<const T*>(p.v) + block * kBlock;
   if (p.src_row) {
     if (token >= p.src_len[p.is_ctx[h] ? 1 : 0]) return;
-    const long long at = ((long long)p.src_row[head] + token) * p.blocks * kBlock;
+    const long long at = ((long long)p.src_row[head] + token) * (BLOCKS * kBlock);
     k += at;
     v += at;
   } else {
@@ -138,35 +162,55 @@ __global__ void __launch_bounds__(kThreads) kv4_append_kernel(const __grid_const
     k += b * p.ks.batch + h * p.ks.head + token * p.ks.token;
     v += b * p.vs.batch + h * p.vs.head + token * p.vs.token;
   }
+  // (read whether or not it has a place: the length is on its way meanwhile)
+  Sixteen<T> rk, rv;
+  rk.load(k, p.whole);
+  rv.load(v, p.whole);
   const long long slot = (long long)max(p.lens[head], 0) + token;
   if (slot >= p.planes.cap) return;
-  Sixteen<T> rk, rv;
-  rk.load(k);
-  rv.load(v);
-  const long long at = (first_row(p.planes, head) + slot) * p.blocks + block;
-  float x[kBlock];
+  const long long at = (first_row(p.planes, head) + slot) * BLOCKS + block;
   uint32_t byte;
-  rk.values(x);
-  uint2 code = quantise(x, byte);
+  uint2 code = quantise(rk, byte);
   reinterpret_cast<uint2*>(p.planes.k_codes)[at] = code;
   p.planes.k_scales[at] = (unsigned char)byte;
-  rv.values(x);
-  code = quantise(x, byte);
+  code = quantise(rv, byte);
   reinterpret_cast<uint2*>(p.planes.v_codes)[at] = code;
   p.planes.v_scales[at] = (unsigned char)byte;
 }
 
-__device__ __forceinline__ void block_values(const uint2& code, uint32_t byte, float* x) {
-  const float s = scale_value(byte);
+// A block's values, in bf16 pairs.
+__device__ __forceinline__ void block_values(const uint2& code, uint32_t byte, uint32_t* w) {
+  const Scale2 s = scale2(byte * 0x10001u);
 #pragma unroll
-  for (int i = 0; i < kBlock; ++i) x[i] = (float)((int)(((i < 8 ? code.x : code.y) >> (4 * (i & 7))) & 15) - 8) * s;
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t c = i ? code.y : code.x;
+    const uint32_t a = values2(c, 0, s), b = values2(c, 4, s), d = values2(c, 8, s), e = values2(c, 12, s);   // (0,4) (1,5) (2,6) (3,7)
+    w[4 * i] = __byte_perm(a, b, 0x5410);
+    w[4 * i + 1] = __byte_perm(d, e, 0x5410);
+    w[4 * i + 2] = __byte_perm(a, b, 0x7632);
+    w[4 * i + 3] = __byte_perm(d, e, 0x7632);
+  }
+}
+template <typename T> __device__ __forceinline__ void store_block(T* dst, const uint32_t* w, bool whole) {
+  if constexpr (sizeof(T) == 2) {
+    ptx::st_global_32b(dst, w, whole);
+  } else {
+    uint32_t x[16];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      x[2 * i] = w[i] << 16;
+      x[2 * i + 1] = w[i] & 0xffff0000u;
+    }
+    ptx::st_global_32b(dst, x, whole);
+    ptx::st_global_32b(dst + 8, x + 8, whole);
+  }
 }
 
-template <typename T>
+template <typename T, int BLOCKS>
 __global__ void __launch_bounds__(kThreads) kv4_read_kernel(const __grid_constant__ RowsParams p) {
   pdl_wait();
   int head, token, block;
-  if (!place(p, head, token, block)) return;
+  if (!place<BLOCKS>(p, head, token, block)) return;
   const int b = head / p.kv_heads, h = head - b * p.kv_heads;
   T* k = static_cast<T*>(const_cast<void*>(p.k)) + b * p.ks.batch + h * p.ks.head + token * p.ks.token + block * kBlock;
   T* v = static_cast<T*>(const_cast<void*>(p.v)) + b * p.vs.batch + h * p.vs.head + token * p.vs.token + block * kBlock;
@@ -174,28 +218,42 @@ __global__ void __launch_bounds__(kThreads) kv4_read_kernel(const __grid_constan
   uint2 kc = make_uint2(0x88888888u, 0x88888888u), vc = kc;      // code 8 stands for 0
   uint32_t kb = 0, vb = 0;
   if (slot >= 0 && slot < p.planes.cap) {
-    const long long at = (first_row(p.planes, head) + slot) * p.blocks + block;
+    const long long at = (first_row(p.planes, head) + slot) * BLOCKS + block;
     kc = reinterpret_cast<const uint2*>(p.planes.k_codes)[at];
     vc = reinterpret_cast<const uint2*>(p.planes.v_codes)[at];
     kb = p.planes.k_scales[at];
     vb = p.planes.v_scales[at];
   }
-  float x[kBlock];
-  block_values(kc, kb, x);
-  Sixteen<T>::store(k, x);
-  block_values(vc, vb, x);
-  Sixteen<T>::store(v, x);
+  uint32_t w[8];
+  block_values(kc, kb, w);
+  store_block(k, w, p.whole);
+  block_values(vc, vb, w);
+  store_block(v, w, p.whole);
 }
 
-template <typename F>
-hack_status_t launch_rows(F* kern, RowsParams& p, int heads, cudaStream_t st) {
-  p.threads = (long long)heads * p.n_tokens * p.blocks;
+bool on_sectors(const void* ptr, const hack_strides_t& s, int elt) {
+  const int unit = 32 / elt;
+  return reinterpret_cast<uintptr_t>(ptr) % 32 == 0 && s.batch % unit == 0 && s.head % unit == 0 && s.token % unit == 0;
+}
+
+// A row's blocks are consecutive threads'.
+hack_status_t launch_rows(bool read, RowsParams& p, int dtype, int head_dim, int heads, cudaStream_t st) {
+  const int blocks = head_dim / kBlock, elt = dtype == HACK_F32 ? 4 : 2;
+  p.threads = (long long)heads * p.n_tokens * blocks;
+  p.whole = on_sectors(p.k, p.ks, elt) && on_sectors(p.v, p.vs, elt);
   const long long grid = (p.threads + kThreads - 1) / kThreads;
   if (grid > 0x7fffffffll) {
     set_error("more rows than a launch has places for");
     return HACK_ERR_UNSUPPORTED;
   }
-  launch_k(kern, dim3((unsigned)grid), dim3(kThreads), 0, st, p);
+  auto go = [&](auto* append, auto* back) { launch_k(read ? back : append, dim3((unsigned)grid), dim3(kThreads), 0, st, p); };
+  if (dtype == HACK_F32) {
+    if (blocks == 4) go(kv4_append_kernel<float, 4>, kv4_read_kernel<float, 4>);
+    else go(kv4_append_kernel<float, 8>, kv4_read_kernel<float, 8>);
+  } else {
+    if (blocks == 4) go(kv4_append_kernel<__nv_bfloat16, 4>, kv4_read_kernel<__nv_bfloat16, 4>);
+    else go(kv4_append_kernel<__nv_bfloat16, 8>, kv4_read_kernel<__nv_bfloat16, 8>);
+  }
   return launched(1) < 0 ? HACK_ERR_CUDA : HACK_OK;
 }
 
@@ -221,7 +279,6 @@ hack_status_t check_rows(const hack_kv4_t* kv, const hack_kv4_rows_t* r, const v
 RowsParams rows_params(const hack_kv4_t* kv) {
   RowsParams p{};
   p.planes = kv4_planes(kv);
-  p.blocks = kv->head_dim / kBlock;
   p.kv_heads = kv->n_kv_heads;
   return p;
 }
@@ -258,8 +315,7 @@ hack_status_t launch_store_kv4(const StepArgs& a, int dtype, const hack_kv4_t* k
   }
   p.n_tokens = longest;
   if (longest == 0) return HACK_OK;
-  return dtype == HACK_F32 ? launch_rows(kv4_append_kernel<float>, p, a.batch * a.n_heads, st)
-                           : launch_rows(kv4_append_kernel<__nv_bfloat16>, p, a.batch * a.n_heads, st);
+  return launch_rows(false, p, dtype, a.head_dim, a.batch * a.n_heads, st);
 }
 
 }  // namespace hack
@@ -278,9 +334,7 @@ extern "C" hack_status_t hack_kv4_append(const hack_kv4_t* kv, const hack_kv4_ro
   p.v = v;
   p.lens = lens;
   p.new_lens = new_lens;
-  const int heads = kv->batch * kv->n_kv_heads;
-  return rows->dtype == HACK_F32 ? launch_rows(kv4_append_kernel<float>, p, heads, (cudaStream_t)stream)
-                                 : launch_rows(kv4_append_kernel<__nv_bfloat16>, p, heads, (cudaStream_t)stream);
+  return launch_rows(false, p, rows->dtype, kv->head_dim, kv->batch * kv->n_kv_heads, (cudaStream_t)stream);
 }
 
 extern "C" hack_status_t hack_kv4_read(const hack_kv4_t* kv, const hack_kv4_rows_t* rows, void* k_out, void* v_out,
@@ -296,7 +350,5 @@ extern "C" hack_status_t hack_kv4_read(const hack_kv4_t* kv, const hack_kv4_rows
   p.k = k_out;
   p.v = v_out;
   p.lens = first;
-  const int heads = kv->batch * kv->n_kv_heads;
-  return rows->dtype == HACK_F32 ? launch_rows(kv4_read_kernel<float>, p, heads, (cudaStream_t)stream)
-                                 : launch_rows(kv4_read_kernel<__nv_bfloat16>, p, heads, (cudaStream_t)stream);
+  return launch_rows(true, p, rows->dtype, kv->head_dim, kv->batch * kv->n_kv_heads, (cudaStream_t)stream);
 }
