@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(F32, NQ)) kv4_attend_ker
   const int len = kv4_length(p, head, nq);
   const int rows = nq * p.group, m0 = tile * ROWS;
   const Kv4Range range = kv4_range(p, len, nq, m0, min(m0 + ROWS, rows) - 1);
-  const int chunks1 = (range.sink_end + kChunk - 1) / kChunk, chunks = m0 < rows ? chunks1 + (range.hi - range.lo + kChunk - 1) / kChunk : 0;
+  const int chunks1 = (range.sink_end + kChunk - 1) / kChunk, chunks = m0 < rows ? kv4_chunks(range, kChunk) : 0;
   const int c_begin = (int)((long long)chunks * split / p.splits), c_end = (int)((long long)chunks * (split + 1) / p.splits);
 
   const uint32_t ring = smem_u32(smem) + warp * Ring<D>::kWarp;

@@ -13,6 +13,7 @@ struct Kv4AttendParams {
   int tile_rows;                    // query rows of a tile: 8 or 16, or 128 on the tensor cores
   int tiles, units, splits;         // tiles of query rows of a stored head, all of them, CTAs that share the rows of one
   int tiles_per_cta;                // tensor cores: 1 or 2
+  int steal;                        // tensor cores: more units than CTAs run at once, a CTA goes on with another one
   int out_sectors;                  // rows of the output start on 32-byte boundaries
   uint32_t wait_polls;              // limit of a wait
   float scale_log2;                 // sm_scale * log2(e)
@@ -49,6 +50,8 @@ __device__ __forceinline__ Kv4Range kv4_range(const Kv4AttendParams& p, int len,
   r.all_sink = p.window > 0 ? p.n_sink : 0;
   return r;
 }
+// Runs of `size` rows that cover it
+__device__ __forceinline__ int kv4_chunks(const Kv4Range& r, int size) { return (r.sink_end + size - 1) / size + (r.hi - r.lo + size - 1) / size; }
 // Whether every query row of the tile sees the 32 rows from `first` on
 __device__ __forceinline__ bool kv4_all_see(const Kv4AttendParams&, const Kv4Range& r, int first) {
   return first + 32 <= r.all_hi && (first >= r.all_lo || first + 32 <= r.all_sink);

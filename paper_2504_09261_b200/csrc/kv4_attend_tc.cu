@@ -1,18 +1,23 @@
 // Attention over a cache of 4 bits on the 5th-generation tensor cores: bf16 queries, many of them to a stored head.
 //
-// A CTA takes one or two tiles of 128 query rows (token * group + head of the group) of a stored head and walks over the
-// blocks of 128 stored rows that they see.  What is multiplied is the stored values themselves, exact in bf16:
+// A unit of work is one or two tiles of 128 query rows (token * group + head of the group) of a stored head, and the blocks of
+// 128 stored rows that they see (or a share of them: `splits`).  What is multiplied is the stored values themselves, exact
+// in bf16:
 //   warps 0, 2   : issue the products Q K^T and P V (a thread each)
-//   warps 4-11   : softmax of the two tiles, one thread per query row; they also put the queries into shared memory
-//   warps 12-15  : read codes and scales, a tile of K or V ahead in registers, and write the values as the operand tiles
+//   warp  1      : finds the CTA's next unit
+//   warps 4-11   : softmax of the two tiles, one thread per query row, and their output
+//   warps 12-15  : queries into shared memory; codes and scales, a tile of K or V ahead in registers, into operand tiles of values
 // A word of eight codes becomes the elements 0 4 1 5 2 6 3 7 of its eight (a shift, a mask and an FMA for two): the order of
 // the elements inside Q K^T is free as long as both sides have it, so the queries are written in it as well, and
 // the columns of P V are put right when the output is written.
 // Tensor memory (512 columns): logits [0,128), one buffer which the tiles take in turn; probabilities [128,192) and [192,256);
 // outputs from 256 on.  A softmax thread reads its logit row into registers and gives the buffer back at once, so that the
 // next Q K^T runs under it; the output is rescaled only when a row's maximum grows by more than 2^32.
+// A CTA that is through with a unit takes over one that has not been launched yet (cluster launch control): its queries and
+// first tiles are on their way under the last softmax and the output of the unit before.
 // Every wait is bounded; a CTA that gives up lets its products end, frees its tensor memory and raises the status word.
 #include <algorithm>
+#include <type_traits>
 
 #include "entry_checks.h"
 #include "kv4_attend.h"
@@ -28,22 +33,85 @@ using namespace kv4;
 using namespace ptx;
 
 constexpr int kBM = 128, kBN = 128;
-constexpr int kQkWarp = 0, kPvWarp = 2, kSoftmaxWarps = 4, kValueWarps = 12;    // first of each role
+constexpr int kQkWarp = 0, kUnitWarp = 1, kPvWarp = 2, kSoftmaxWarps = 4, kValueWarps = 12;    // first of each role
 constexpr int kThreads = 512;
-// 256 * 200 + 128 * 72 + 128 * 40 registers = 512 * 128
-constexpr int kSoftmaxRegs = 200, kValueRegs = 72, kIssueRegs = 40;
+// 256 * 184 + 128 * 96 + 128 * 48 registers = 512 * 128
+constexpr int kSoftmaxRegs = 184, kValueRegs = 96, kIssueRegs = 48;
 constexpr int kStages = 2;
 constexpr float kRaise = 32.f;               // log2 by which a logit may exceed the reference maximum
 constexpr uint32_t kDrainPolls = 1u << 22;
+constexpr int kShortUnit = 16;               // blocks below which the next unit is asked for at the start of one
+
+// A unit of work, in shared memory.  (Worked out by one thread for all roles: the same code in each of them was 10 % of the largest
+// launch's time, in waits for instructions.)
+struct Unit {
+  long long row0;                            // first row of the stored head
+  int more;                                  // 0: there is no unit any more
+  int b, kvh, head;                          // the stored head
+  int len, nq, rows, m0, ntile;              // its length, tokens and query rows; first row and tiles of the unit (0: nothing to do)
+  int tile, split;                           // number of its first tile in the head; share of the blocks
+  int blocks1, j_begin, nblk;                // blocks of the first run of rows, [0, sink_end); the unit's blocks
+  int lo, hi, sink_end, all_lo, all_hi, all_sink;   // Kv4Range
+};
 
 struct Bars {
-  uint64_t q_full[2];
+  uint4 answer;                              // of cluster launch control
+  Unit unit[2];                              // units of even and odd count
+  uint64_t u_full[2], u_empty[2], asked;
+  uint64_t q_full[2], q_free[2];
   uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
   uint64_t s_full[2], s_free, p_full[2], p_free[2];
   uint64_t drain[2];
   uint32_t tmem_base;
   int gave_up;
 };
+
+// Unit number x of the launch; x < 0: there is no more.
+__device__ __forceinline__ void make_unit(const Kv4AttendParams& p, int x, volatile Unit& u) {
+  u.more = x >= 0;
+  u.ntile = u.nblk = 0;
+  if (x < 0) return;
+  const int heads = p.units / p.tiles, per = p.tiles_per_cta, cta_units = (p.tiles + per - 1) / per;
+  const int split = x % p.splits;
+  x /= p.splits;
+  const int head = x % heads, tile = (cta_units - 1 - x / heads) * per;   // the last tiles, of a causal call the longest, come first
+  const int b = head / p.kv_heads;
+  const int nq = p.new_lens ? min(max(p.new_lens[b], 0), p.n_queries) : p.n_queries;
+  const int rows = nq * p.group, m0 = tile * kBM;
+  if (m0 >= rows) return;                    // queries of a padded batch that it does not have
+  const int len = kv4_length(p, head, nq);
+  const Kv4Range r = kv4_range(p, len, nq, m0, min(m0 + per * kBM, rows) - 1);
+  const uint32_t blocks = kv4_chunks(r, kBN), begin = blocks * split / p.splits;
+  u.row0 = first_row(p.planes, head);
+  u.b = b;
+  u.kvh = head - b * p.kv_heads;
+  u.head = head;
+  u.len = len;
+  u.nq = nq;
+  u.rows = rows;
+  u.m0 = m0;
+  u.ntile = per == 2 && m0 + kBM < rows ? 2 : 1;
+  u.tile = tile;
+  u.split = split;
+  u.blocks1 = (r.sink_end + kBN - 1) / kBN;
+  u.j_begin = begin;
+  u.nblk = blocks * (split + 1) / p.splits - begin;
+  u.lo = r.lo;
+  u.hi = r.hi;
+  u.sink_end = r.sink_end;
+  u.all_lo = r.all_lo;
+  u.all_hi = r.all_hi;
+  u.all_sink = r.all_sink;
+}
+// Block j of a unit: its first stored row and the end of the rows that count
+__device__ __forceinline__ void block_at(const volatile Unit& u, int j, int& first, int& end) {
+  j += u.j_begin;
+  const int blocks1 = u.blocks1;
+  first = j < blocks1 ? j * kBN : u.lo + (j - blocks1) * kBN;
+  end = j < blocks1 ? u.sink_end : u.hi;
+}
+// Bits below n
+__device__ __forceinline__ uint32_t bits_below(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
 
 __device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, Bars* b, uint32_t polls) {
   const uint32_t addr = smem_u32(bar);
@@ -70,34 +138,18 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid
   const uint32_t polls = p.wait_polls;
 
   pdl_grid_wait();
-  // Heads inside units of the same place: the last tiles, of a causal call the longest, come first
-  const int split = blockIdx.x % p.splits, at = blockIdx.x / p.splits;
-  const int heads = p.units / p.tiles, per = p.tiles_per_cta, cta_units = (p.tiles + per - 1) / per;
-  const int head = at % heads, cta_unit = cta_units - 1 - at / heads;
-  const int b = head / p.kv_heads, kvh = head - b * p.kv_heads;
-  const int nq = p.new_lens ? min(max(p.new_lens[b], 0), p.n_queries) : p.n_queries;
-  const int rows = nq * p.group, m0 = cta_unit * per * kBM;
-  if (m0 >= rows) return;                    // (the queries of a padded batch that it does not have)
-  const int ntile = per == 2 && m0 + kBM < rows ? 2 : 1;
-  const int len = kv4_length(p, head, nq);
-  const Kv4Range range = kv4_range(p, len, nq, m0, min(m0 + per * kBM, rows) - 1);
-  const int blocks1 = (range.sink_end + kBN - 1) / kBN, blocks = blocks1 + (range.hi - range.lo + kBN - 1) / kBN;
-  const int j_begin = (int)((long long)blocks * split / p.splits), j_end = (int)((long long)blocks * (split + 1) / p.splits);
-  const int nblk = j_end - j_begin;
-  auto block_at = [&](int j, int& first, int& end) {
-    first = j < blocks1 ? j * kBN : range.lo + (j - blocks1) * kBN;
-    end = j < blocks1 ? range.sink_end : range.hi;
-  };
-
   if (tid == 0) {
     for (int t = 0; t < 2; ++t) {
-      mbar_init(smem_u32(&bars->q_full[t]), 4);          // an arrival of each warp of the tile
+      mbar_init(smem_u32(&bars->u_full[t]), 1);
+      mbar_init(smem_u32(&bars->u_empty[t]), 14);      mbar_init(smem_u32(&bars->q_full[t]), 4);
+      mbar_init(smem_u32(&bars->q_free[t]), 1);
       mbar_init(smem_u32(&bars->s_full[t]), 1);
       mbar_init(smem_u32(&bars->p_full[t]), 4);
       mbar_init(smem_u32(&bars->p_free[t]), 1);
       mbar_init(smem_u32(&bars->drain[t]), 1);
     }
-    mbar_init(smem_u32(&bars->s_free), 4);
+    mbar_init(smem_u32(&bars->asked), 1);
+    mbar_init(smem_u32(&bars->s_free), 4);               // the warps of the tile whose logits were in the buffer
     for (int s = 0; s < kStages; ++s) {
       mbar_init(smem_u32(&bars->k_full[s]), 4);
       mbar_init(smem_u32(&bars->k_empty[s]), 1);
@@ -108,6 +160,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid
     fence_barrier_init();
     fence_proxy_async();
   }
+  if (tid == kUnitWarp * 32) make_unit(p, blockIdx.x, bars->unit[0]);
   if (warp == kQkWarp) {
     __syncwarp();
     tmem_alloc(smem_u32(&bars->tmem_base), 512);
@@ -120,17 +173,23 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid
   tc_fence_after();
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&bars->tmem_base);
 
+  // A role takes unit number n of the CTA (the first is ready, the others warp 1 makes), and gives it back.  False: a wait gave up.
+  auto take_unit = [&](int n) { return n == 0 || wait_bar(&bars->u_full[n & 1], ((n - 1) >> 1) & 1, bars, polls); };
+  auto give_unit = [&](int n) { mbar_arrive(smem_u32(&bars->u_empty[n & 1])); };
+
   if (warp >= kValueWarps) {
     // ------------------------------------------------------------------ codes to values
     reg_dec<kValueRegs>();
     constexpr int LPR = D / 32, RPW = 32 / LPR, PASSES = kBN / (4 * RPW);   // lanes of a row (16 bytes of codes each), rows of a warp
     const int t = lane % LPR, row_in = (warp - kValueWarps) * RPW + lane / LPR;
-    const long long row0 = first_row(p.planes, head);
     uint4 codes[2][PASSES];
     uint32_t scales[2][PASSES];
+    uint32_t g = 0;                            // blocks of the units before
+    const volatile Unit* unit = bars->unit;
+    long long row0 = 0;
     auto load = [&](int item, int set) {       // item 2 j: keys of block j, 2 j + 1: its values
       int first, end;
-      block_at(j_begin + (item >> 1), first, end);
+      block_at(*unit, item >> 1, first, end);
       const unsigned char* c = item & 1 ? p.planes.v_codes : p.planes.k_codes;
       const unsigned char* s = item & 1 ? p.planes.v_scales : p.planes.k_scales;
 #pragma unroll
@@ -141,16 +200,14 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid
         scales[set][i] = *reinterpret_cast<const uint16_t*>(s + row * (D / 16) + t * 2);
       }
     };
-    auto write = [&](int item, int set) {
-      const int j = item >> 1, slot = j % kStages;
-      const uint32_t tile = (item & 1 ? v_sm : k_sm) + slot * TILE_BYTES;
+    auto write = [&](uint32_t tile, int set) {
 #pragma unroll
       for (int i = 0; i < PASSES; ++i) {
         const int row = i * 4 * RPW + row_in;
-        const uint4 u = codes[set][i];
+        const uint4 c = codes[set][i];
         // eight lanes write eight different 16-byte columns: those of the second 64 elements take their words in another order
         const bool other = D == 128 && (t & 2);
-        const uint32_t w[4] = {other ? u.z : u.x, other ? u.w : u.y, other ? u.x : u.z, other ? u.y : u.w};
+        const uint32_t w[4] = {other ? c.z : c.x, other ? c.w : c.y, other ? c.x : c.z, other ? c.y : c.w};
         const uint32_t lo = scales[set][i] & 0xff, hi = scales[set][i] >> 8;
         const Scale2 s0 = scale2((other ? hi : lo) * 0x10001u), s1 = scale2((other ? lo : hi) * 0x10001u);
 #pragma unroll
@@ -163,57 +220,109 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid
         }
       }
     };
-    auto turn = [&](int item, int set) {
-      if (item + 1 < 2 * nblk) load(item + 1, set ^ 1);
-      const int j = item >> 1, slot = j % kStages;
-      if (j >= kStages &&
-          !__all_sync(0xffffffffu, wait_bar(item & 1 ? &bars->v_empty[slot] : &bars->k_empty[slot], (j / kStages - 1) & 1, bars, polls)))
-        return false;
-      write(item, set);
-      fence_proxy_async();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(item & 1 ? &bars->v_full[slot] : &bars->k_full[slot]));
-      return true;
-    };
-    if (nblk > 0) load(0, 0);
-#pragma unroll 1
-    for (int j = 0; j < nblk; ++j)
-      if (!turn(2 * j, 0) || !turn(2 * j + 1, 1)) break;
-  } else if (warp >= kSoftmaxWarps) {
-    // ------------------------------------------------------------------ queries, softmax, output
-    reg_inc<kSoftmaxRegs>();
-    const int t = (warp - kSoftmaxWarps) >> 2, row = tid & 127;
-    if (t < ntile) {
-      const int m = m0 + t * kBM + row, token = m / p.group;
-      const bool live = m < rows;
-      const long long q_at = b * p.q_stride.batch + (long long)(kvh * p.group + m - token * p.group) * p.q_stride.head +
-                             (long long)token * p.q_stride.token;
+    uint32_t q_loads[2] = {0, 0};
+    // a tile of queries, a row a thread
+    auto queries = [&](int tile) {
+      const int row = tid & 127, m = unit->m0 + tile * kBM + row, token = m / p.group;
+      const bool live = m < unit->rows;
+      const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + unit->b * p.q_stride.batch +
+                                                        (long long)(unit->kvh * p.group + m - token * p.group) * p.q_stride.head +
+                                                        (long long)token * p.q_stride.token);
+      if (q_loads[tile] > 0 && !__all_sync(0xffffffffu, wait_bar(&bars->q_free[tile], (q_loads[tile] - 1) & 1, bars, polls))) return false;
 #pragma unroll 4
       for (int chunk = 0; chunk < D / 8; ++chunk) {
-        const uint4 v = live ? reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + q_at)[chunk] : make_uint4(0, 0, 0, 0);
-        const uint32_t dst = q_sm + t * TILE_BYTES + (chunk >> 3) * SUB_BYTES + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
+        const uint4 v = live ? src[chunk] : make_uint4(0, 0, 0, 0);
+        const uint32_t dst = q_sm + tile * TILE_BYTES + (chunk >> 3) * SUB_BYTES + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(__byte_perm(v.x, v.z, 0x5410)), "r"(__byte_perm(v.x, v.z, 0x7632)),
                      "r"(__byte_perm(v.y, v.w, 0x5410)), "r"(__byte_perm(v.y, v.w, 0x7632)) : "memory");
       }
       fence_proxy_async();
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&bars->q_full[t]));
-
-      const uint32_t lane_addr = static_cast<uint32_t>((warp & 3) * 32) << 16;
-      const uint32_t s_addr = tmem + lane_addr + S_COL, p_addr = tmem + lane_addr + P_COL + t * 64, o_addr = tmem + lane_addr + O_COL + t * D;
-      const float c = p.scale_log2;
+      if (lane == 0) mbar_arrive(smem_u32(&bars->q_full[tile]));
+      ++q_loads[tile];
+      return true;
+    };
+    auto turn = [&](auto keys, int j, int set, int nblk) {
+      constexpr bool K = decltype(keys)::value;
+      const int item = 2 * j + (K ? 0 : 1);
+      if (item + 1 < 2 * nblk) load(item + 1, set ^ 1);
+      const uint32_t n = g + j, slot = n % kStages;
+      if (n >= kStages &&
+          !__all_sync(0xffffffffu, wait_bar(K ? &bars->k_empty[slot] : &bars->v_empty[slot], (n / kStages - 1) & 1, bars, polls)))
+        return false;
+      write((K ? k_sm : v_sm) + slot * TILE_BYTES, set);
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(K ? &bars->k_full[slot] : &bars->v_full[slot]));
+      return true;
+    };
+    bool ok = true;
+#pragma unroll 1
+    for (int n = 0; ok; ++n) {
+      ok = __all_sync(0xffffffffu, take_unit(n));
+      if (!ok) break;
+      unit = &bars->unit[n & 1];
+      const int nblk = unit->nblk;
+      if (!unit->more) break;
+      if (nblk > 0) {
+        row0 = unit->row0;
+        load(0, 0);
+        ok = queries(0) && (unit->ntile == 1 || queries(1));
+#pragma unroll 1
+        for (int j = 0; j < nblk && ok; ++j) ok = turn(std::true_type(), j, 0, nblk) && turn(std::false_type(), j, 1, nblk);
+        g += nblk;
+      }
+      __syncwarp();
+      if (lane == 0) give_unit(n);
+    }
+  } else if (warp >= kSoftmaxWarps) {
+    // ------------------------------------------------------------------ softmax, output
+    reg_inc<kSoftmaxRegs>();
+    const int t = (warp - kSoftmaxWarps) >> 2, row = tid & 127;
+    const uint32_t lane_addr = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t s_addr = tmem + lane_addr + S_COL, p_addr = tmem + lane_addr + P_COL + t * 64, o_addr = tmem + lane_addr + O_COL + t * D;
+    const float c = p.scale_log2;
+    uint32_t cnt = 0;                          // blocks of this tile so far
+    bool ok = true;
+    auto bar_all = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_bar(bar, parity, bars, polls)) != 0; };
+#pragma unroll 1
+    for (int n = 0; ok; ++n) {
+      ok = __all_sync(0xffffffffu, take_unit(n));
+      if (!ok) break;
+      const volatile Unit& u = bars->unit[n & 1];                  // (registers that live through a block are scarce)
+      if (!u.more) break;
+      if (t >= u.ntile) {
+        __syncwarp();
+        if (lane == 0) give_unit(n);
+        continue;
+      }
+      const int nblk = u.nblk;
       float m_used = kNoLogit, l = 0.f;
-      bool ok = true;
-      auto bar_all = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_bar(bar, parity, bars, polls)) != 0; };
-      const int pos = len - nq + token;
-      const int see_hi = p.causal ? min(len, pos + 1) : len, see_lo = p.window > 0 ? pos - p.window + 1 : 0;
 #pragma unroll 1
       for (int j = 0; j < nblk; ++j) {
-        int first, end;
-        block_at(j_begin + j, first, end);
-        ok = bar_all(&bars->s_full[t], j & 1);
+        ok = bar_all(&bars->s_full[t], cnt & 1);
         if (!ok) break;
         tc_fence_after();
+        int first, end;
+        block_at(u, j, first, end);
+        if (__builtin_expect(first + kBN > min(end, u.all_hi) || !(first >= u.all_lo || first + kBN <= u.all_sink), 0)) {
+          // Hidden logits become -inf where they are, 32 rows at a time as bits.  (On all 128 in registers, with three comparisons
+          // for each, it took 4 us a block, and the code slowed down the blocks that do not run it.)
+          const int pos = u.len - u.nq + (u.m0 + t * kBM + row) / p.group;
+          const int hi = min(end, p.causal ? pos + 1 : end) - first;
+          const int lo = (p.window > 0 ? pos - p.window + 1 : 0) - first, sink = u.all_sink - first;
+#pragma unroll 1
+          for (int ch = 0; ch < 4; ++ch) {
+            const uint32_t keep = bits_below(hi - 32 * ch) & (~bits_below(lo - 32 * ch) | bits_below(sink - 32 * ch));
+            uint32_t z[32];
+            tmem_ld32(s_addr + ch * 32, z);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) z[i] = keep & (1u << i) ? z[i] : 0xff800000u;
+            tmem_st32(s_addr + ch * 32, z);
+          }
+          tmem_wait_st();
+        }
         uint32_t sr[kBN];
 #pragma unroll
         for (int ch = 0; ch < 4; ++ch) tmem_ld32(s_addr + ch * 32, sr + ch * 32);
@@ -221,18 +330,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&bars->s_free));       // the logits are in registers
-        if (__builtin_expect(first + kBN > min(end, range.all_hi) || !(first >= range.all_lo || first + kBN <= range.all_sink), 0)) {
-          const int hi = min(end, see_hi) - first, lo = see_lo - first, sink = (p.window > 0 ? p.n_sink : 0) - first;
-#pragma unroll
-          for (int i = 0; i < kBN; ++i)
-            if (i >= hi || (i < lo && i >= sink)) sr[i] = 0xff800000u;   // -inf
-        }
         float mx4[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          mx4[u] = -INFINITY;
+        for (int v = 0; v < 4; ++v) {
+          mx4[v] = -INFINITY;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) mx4[u] = max3(mx4[u], __uint_as_float(sr[u * 32 + 2 * i]), __uint_as_float(sr[u * 32 + 2 * i + 1]));
+          for (int i = 0; i < 16; ++i) mx4[v] = max3(mx4[v], __uint_as_float(sr[v * 32 + 2 * i]), __uint_as_float(sr[v * 32 + 2 * i + 1]));
         }
         const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
         const bool grow = (mx - m_used) * c > kRaise;              // in the first block that the row sees anything of
@@ -251,21 +354,18 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid
         uint32_t pk[kBN / 2];
 #pragma unroll
         for (int i = 0; i < kBN / 2; ++i) {
-          const float2 x = fma2(make_float2(__uint_as_float(sr[2 * i]), __uint_as_float(sr[2 * i + 1])), c2, nmc2);
-          float2 pr;
-          pr.x = ex2(x.x);
-          pr.y = ex2(x.y);
-          const __nv_bfloat162 hh = __floats2bfloat162_rn(pr.x, pr.y);
+          const float2 z = fma2(make_float2(__uint_as_float(sr[2 * i]), __uint_as_float(sr[2 * i + 1])), c2, nmc2);
+          const __nv_bfloat162 hh = __floats2bfloat162_rn(ex2(z.x), ex2(z.y));
           pk[i] = *reinterpret_cast<const uint32_t*>(&hh);
           add_bf162(sum[2 * (i & 1)], sum[2 * (i & 1) + 1], pk[i]);
         }
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        if (j > 0) {
+        if (cnt > 0) {
           // the product of the block before still reads P_t and adds to O_t
-          ok = bar_all(&bars->p_free[t], (j - 1) & 1);
+          ok = bar_all(&bars->p_free[t], (cnt - 1) & 1);
           if (!ok) break;
           tc_fence_after();
-          if (any) {
+          if (any && j > 0) {
 #pragma unroll 1
             for (int ch = 0; ch < D / 8; ++ch) {
               uint32_t orr[8];
@@ -283,57 +383,60 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&bars->p_full[t]));
+        ++cnt;
       }
       if (ok && nblk > 0) {
-        ok = bar_all(&bars->p_free[t], (nblk - 1) & 1);
+        ok = bar_all(&bars->p_free[t], (cnt - 1) & 1);             // the unit's last product
         tc_fence_after();
       }
-      if (ok) {
-        const int g = m - token * p.group;
-        const float inv = l > 0.f ? 1.f / l : 0.f;
-        unsigned char* dst = nullptr;
-        float* part = nullptr;
-        if (p.splits > 1) {
-          const long long unit = (long long)head * p.tiles + cta_unit * per + t;
-          float* const at_split = p.partial + (unit * p.splits + split) * (kBM * (D + 2));
-          part = at_split + row * D;
-          if (live) *reinterpret_cast<float2*>(at_split + kBM * D + 2 * row) = make_float2(m_used, l);
-        } else {
-          dst = reinterpret_cast<unsigned char*>(static_cast<__nv_bfloat16*>(p.out) + b * p.out_stride.batch +
-                                                 (long long)(kvh * p.group + g) * p.out_stride.head + (long long)token * p.out_stride.token);
-        }
+      if (!ok) break;
+      const float inv = l > 0.f ? 1.f / l : 0.f;
+      const int tile = u.tile + t, m = tile * kBM + row, token = m / p.group;
+      const bool live = m < u.rows;
+      unsigned char* dst = nullptr;
+      float* part = nullptr;
+      if (p.splits > 1) {
+        float* const at_split = p.partial + (((long long)u.head * p.tiles + tile) * p.splits + u.split) * (kBM * (D + 2));
+        part = at_split + row * D;
+        if (live) *reinterpret_cast<float2*>(at_split + kBM * D + 2 * row) = make_float2(m_used, l);
+      } else {
+        dst = reinterpret_cast<unsigned char*>(static_cast<__nv_bfloat16*>(p.out) + u.b * p.out_stride.batch +
+                                               (long long)(u.kvh * p.group + m - token * p.group) * p.out_stride.head +
+                                               (long long)token * p.out_stride.token);
+      }
 #pragma unroll 1
-        for (int ch = 0; ch < D / 16; ++ch) {
-          uint32_t o[16];
-          if (nblk > 0) {
-            tmem_ld16(o_addr + ch * 16, o);
-            tmem_wait_ld();
-          } else {
+      for (int ch = 0; ch < D / 16; ++ch) {
+        uint32_t o[16];
+        if (nblk > 0) {
+          tmem_ld16(o_addr + ch * 16, o);
+          tmem_wait_ld();
+        } else {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[i] = 0;
+          for (int i = 0; i < 16; ++i) o[i] = 0;
+        }
+        // columns 0 4 1 5 2 6 3 7 of every eight
+        float y[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) y[i] = __uint_as_float(o[(i & 8) + 2 * (i & 3) + ((i >> 2) & 1)]);
+        if (!live) continue;
+        if (part) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) reinterpret_cast<float4*>(part + ch * 16)[i] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+        } else {
+          uint32_t w[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const __nv_bfloat162 hh = __floats2bfloat162_rn(y[2 * i] * inv, y[2 * i + 1] * inv);
+            w[i] = *reinterpret_cast<const uint32_t*>(&hh);
           }
-          // columns 0 4 1 5 2 6 3 7 of every eight
-          float x[16];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) x[i] = __uint_as_float(o[(i & 8) + 2 * (i & 3) + ((i >> 2) & 1)]);
-          if (!live) continue;
-          if (part) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) reinterpret_cast<float4*>(part + ch * 16)[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
-          } else {
-            uint32_t w[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const __nv_bfloat162 hh = __floats2bfloat162_rn(x[2 * i] * inv, x[2 * i + 1] * inv);
-              w[i] = *reinterpret_cast<const uint32_t*>(&hh);
-            }
-            st_global_32b(dst + ch * 32, w, p.out_sectors != 0);
-          }
+          st_global_32b(dst + ch * 32, w, p.out_sectors != 0);
         }
       }
+      tc_fence_before();                                           // (the next unit's products write there)
+      __syncwarp();
+      if (lane == 0) give_unit(n);
     }
   } else {
-    // ------------------------------------------------------------------ issuers of the products
     reg_dec<kIssueRegs>();
     // An issuer leaves when its last product has ended, or after a while
     auto drained = [&](uint64_t* bar) {
@@ -341,49 +444,110 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid
 #pragma unroll 1
       for (uint32_t it = 0; it < kDrainPolls && !mbar_try_wait(smem_u32(bar), 0); ++it) {}
     };
-    if (warp == kQkWarp && lane == 0) {
+    bool ok = true;
+    if (warp == kUnitWarp && lane == 0) {
+      // ---------------------------------------------------------------- the CTA's next unit
+      uint32_t q_loads = 0, answers = 0;                           // units with products, of this CTA; answers
+      bool asked = false;
+#pragma unroll 1
+      for (int n = 0; ok; ++n) {
+        int next = -1;
+        if (p.steal) {
+          // asked for at the start of a short unit, of a long one behind its last product with the first tile's queries
+          // (asked for earlier, it would be kept from CTAs that are idle by then)
+          const int nblk = bars->unit[n & 1].nblk;
+          if (nblk >= kShortUnit) ok = wait_bar(&bars->q_free[0], q_loads & 1, bars, polls);
+          if (nblk > 0) ++q_loads;
+          if (!ok) break;
+          mbar_expect_tx(smem_u32(&bars->asked), 16);
+          clc_ask(smem_u32(&bars->answer), smem_u32(&bars->asked));
+          asked = true;
+          ok = wait_bar(&bars->asked, answers & 1, bars, polls);
+          if (!ok) break;
+          asked = false;
+          ++answers;
+          next = clc_answer(smem_u32(&bars->answer));
+          fence_proxy_async();                                     // the next answer overwrites what was just read
+        }
+        const int slot = (n + 1) & 1;
+        // (unit n - 1 has been given back)
+        if (n >= 1) ok = wait_bar(&bars->u_empty[slot], ((n - 1) >> 1) & 1, bars, polls);
+        if (!ok) break;
+        make_unit(p, next, bars->unit[slot]);
+        mbar_arrive(smem_u32(&bars->u_full[slot]));
+        if (next < 0) break;
+      }
+      if (asked) {                                                 // an answer on its way gets a bounded chance to land
+#pragma unroll 1
+        for (uint32_t it = 0; it < kDrainPolls && !mbar_try_wait(smem_u32(&bars->asked), answers & 1); ++it) {}
+      }
+    } else if (warp == kQkWarp && lane == 0) {
+      // ---------------------------------------------------------------- issuer of Q K^T
       constexpr uint32_t IDESC = idesc_bf16_f32(kBM, kBN, 0);
       const uint64_t q_desc = smem_desc_sw128(q_sm, 16, 1024), k_desc = smem_desc_sw128(k_sm, 16, 1024);
-      bool ok = true;
-      uint32_t use = 0;                                  // products issued
+      uint32_t use = 0, g = 0, q_odd = 0;                          // products issued; blocks of the units before; parity of the tiles' queries
 #pragma unroll 1
-      for (int j = 0; j < nblk && ok; ++j) {
-        const uint32_t slot = j % kStages;
-        const uint64_t kd = k_desc + (uint64_t)((slot * TILE_BYTES) >> 4);
+      for (int n = 0; ok; ++n) {
+        ok = take_unit(n);
+        if (!ok) break;
+        const int nblk = bars->unit[n & 1].nblk, ntile = bars->unit[n & 1].ntile, more = bars->unit[n & 1].more;
+        give_unit(n);
+        if (!more) break;
 #pragma unroll 1
-        for (int t = 0; t < ntile; ++t) {
-          if (j == 0) ok = wait_bar(&bars->q_full[t], 0, bars, polls);
-          if (ok && t == 0) ok = wait_bar(&bars->k_full[slot], (j / kStages) & 1, bars, polls);
-          if (!ok || !wait_bar(&bars->s_free, (use - 1) & 1, bars, polls)) { ok = false; break; }   // (a fresh barrier passes for odd)
-          tc_fence_after();
-          const uint64_t qd = q_desc + (uint64_t)((t * TILE_BYTES) >> 4);
-          if constexpr (D == 128) mma_ss_chain8(tmem + S_COL, qd, kd, IDESC, 0);
-          else mma_ss_chain4(tmem + S_COL, qd, kd, IDESC, 0);
-          mma_commit(smem_u32(&bars->s_full[t]));
-          ++use;
+        for (int j = 0; j < nblk && ok; ++j) {
+          const uint32_t slot = (g + j) % kStages;
+          const uint64_t kd = k_desc + (uint64_t)((slot * TILE_BYTES) >> 4);
+#pragma unroll 1
+          for (int t = 0; t < ntile; ++t) {
+            if (j == 0) {
+              ok = wait_bar(&bars->q_full[t], (q_odd >> t) & 1, bars, polls);
+              q_odd ^= 1u << t;
+            }
+            if (ok && t == 0) ok = wait_bar(&bars->k_full[slot], ((g + j) / kStages) & 1, bars, polls);
+            if (!ok || !wait_bar(&bars->s_free, (use - 1) & 1, bars, polls)) { ok = false; break; }   // (a fresh barrier passes for odd)
+            tc_fence_after();
+            const uint64_t qd = q_desc + (uint64_t)((t * TILE_BYTES) >> 4);
+            if constexpr (D == 128) mma_ss_chain8(tmem + S_COL, qd, kd, IDESC, 0);
+            else mma_ss_chain4(tmem + S_COL, qd, kd, IDESC, 0);
+            mma_commit(smem_u32(&bars->s_full[t]));
+            ++use;
+            if (j == nblk - 1) mma_commit(smem_u32(&bars->q_free[t]));
+          }
+          if (ok) mma_commit(smem_u32(&bars->k_empty[slot]));
         }
-        if (ok) mma_commit(smem_u32(&bars->k_empty[slot]));
+        g += nblk;
       }
       drained(&bars->drain[0]);
     } else if (warp == kPvWarp && lane == 0) {
-      constexpr uint32_t IDESC = idesc_bf16_f32(kBM, D, 1);          // V: rows of the tile are the summed index
+      // ---------------------------------------------------------------- issuer of P V
+      constexpr uint32_t IDESC = idesc_bf16_f32(kBM, D, 1);        // V: rows of the tile are the summed index
       const uint64_t v_desc = smem_desc_sw128(v_sm, SUB_BYTES, 1024);
-      bool ok = true;
+      uint32_t g = 0, odd = 0;                                     // blocks of the units before; parity of the tiles' products
 #pragma unroll 1
-      for (int j = 0; j < nblk && ok; ++j) {
-        const uint32_t slot = j % kStages;
-        const uint64_t vd = v_desc + (uint64_t)((slot * TILE_BYTES) >> 4);
+      for (int n = 0; ok; ++n) {
+        ok = take_unit(n);
+        if (!ok) break;
+        const int nblk = bars->unit[n & 1].nblk, ntile = bars->unit[n & 1].ntile, more = bars->unit[n & 1].more;
+        give_unit(n);
+        if (!more) break;
 #pragma unroll 1
-        for (int t = 0; t < ntile; ++t) {
-          if (t == 0) ok = wait_bar(&bars->v_full[slot], (j / kStages) & 1, bars, polls);
-          if (!ok || !wait_bar(&bars->p_full[t], j & 1, bars, polls)) { ok = false; break; }
-          tc_fence_after();
-          const uint32_t o = tmem + O_COL + t * D, pa = tmem + P_COL + t * 64;
-          mma_ts_chain4(o, pa, vd, IDESC, j > 0);
-          mma_ts_chain4(o, pa + 32, vd + 4 * 128, IDESC, 1);
-          mma_commit(smem_u32(&bars->p_free[t]));
+        for (int j = 0; j < nblk && ok; ++j) {
+          const uint32_t slot = (g + j) % kStages;
+          const uint64_t vd = v_desc + (uint64_t)((slot * TILE_BYTES) >> 4);
+#pragma unroll 1
+          for (int t = 0; t < ntile; ++t) {
+            if (t == 0) ok = wait_bar(&bars->v_full[slot], ((g + j) / kStages) & 1, bars, polls);
+            if (!ok || !wait_bar(&bars->p_full[t], (odd >> t) & 1, bars, polls)) { ok = false; break; }
+            odd ^= 1u << t;
+            tc_fence_after();
+            const uint32_t o = tmem + O_COL + t * D, pa = tmem + P_COL + t * 64;
+            mma_ts_chain4(o, pa, vd, IDESC, j > 0);
+            mma_ts_chain4(o, pa + 32, vd + 4 * 128, IDESC, 1);
+            mma_commit(smem_u32(&bars->p_free[t]));
+          }
+          if (ok) mma_commit(smem_u32(&bars->v_empty[slot]));
         }
-        if (ok) mma_commit(smem_u32(&bars->v_empty[slot]));
+        g += nblk;
       }
       drained(&bars->drain[1]);
     }
@@ -400,13 +564,15 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid
 template <int D> constexpr size_t smem_bytes() { return 1024 + (2 + 2 * kStages) * (size_t)(D / 64) * kBN * 128 + sizeof(Bars) + 64; }
 
 template <int D>
-int launch(const Kv4AttendParams& p, cudaStream_t st) {
+int launch(Kv4AttendParams p, cudaStream_t st) {
   // (more than half of an SM's shared memory at head_dim 64 as well: a CTA owns the SM's tensor memory)
   constexpr size_t smem = smem_bytes<128>();
   static_assert(smem_bytes<D>() <= smem, "");
   if (!allow_dynamic_smem(kv4_attend_tc_kernel<D>, smem)) return -1;
   const int heads = p.units / p.tiles, cta_units = (p.tiles + p.tiles_per_cta - 1) / p.tiles_per_cta;
-  launch_k(kv4_attend_tc_kernel<D>, dim3((unsigned)((long long)heads * cta_units * p.splits)), dim3(kThreads), smem, st, p);
+  const int grid = heads * cta_units * p.splits;
+  p.steal = grid > sm_count();               // more units than CTAs run at once
+  launch_k(kv4_attend_tc_kernel<D>, dim3(grid), dim3(kThreads), smem, st, p);
   return launched(1);
 }
 
