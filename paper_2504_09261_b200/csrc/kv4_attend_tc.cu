@@ -103,13 +103,6 @@ __device__ __forceinline__ void make_unit(const Kv4AttendParams& p, int x, volat
   u.all_hi = r.all_hi;
   u.all_sink = r.all_sink;
 }
-// Block j of a unit: its first stored row and the end of the rows that count
-__device__ __forceinline__ void block_at(const volatile Unit& u, int j, int& first, int& end) {
-  j += u.j_begin;
-  const int blocks1 = u.blocks1;
-  first = j < blocks1 ? j * kBN : u.lo + (j - blocks1) * kBN;
-  end = j < blocks1 ? u.sink_end : u.hi;
-}
 // Bits below n
 __device__ __forceinline__ uint32_t bits_below(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
 
@@ -123,6 +116,23 @@ __device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, Bars* b
     if (polls == 0) { *flag = 1; return false; }
   }
   return true;
+}
+
+// Logits of a row that its query does not see become -inf where they are: columns from hi on, and those below lo from sink on.  32 at
+// a time, as bits.  (On all 128 in registers, with three comparisons for each, it took 4 us a block.)
+__device__ __forceinline__ void hide(uint32_t s_addr, int hi, int lo, int sink) {
+#pragma unroll 1
+  for (int ch = 0; ch < kBN / 32; ++ch) {
+    const uint32_t keep = bits_below(hi - 32 * ch) & (~bits_below(lo - 32 * ch) | bits_below(sink - 32 * ch));
+    if (__all_sync(0xffffffffu, keep == ~0u)) continue;
+    uint32_t z[32];
+    tmem_ld32(s_addr + ch * 32, z);
+    tmem_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 32; ++i) z[i] = keep & (1u << i) ? z[i] : 0xff800000u;
+    tmem_st32(s_addr + ch * 32, z);
+  }
+  tmem_wait_st();
 }
 
 template <int D>
@@ -187,9 +197,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid
     uint32_t g = 0;                            // blocks of the units before
     const volatile Unit* unit = bars->unit;
     long long row0 = 0;
+    int j_begin = 0, blocks1 = 0, lo = 0, hi = 0, sink_end = 0;        // of the unit
     auto load = [&](int item, int set) {       // item 2 j: keys of block j, 2 j + 1: its values
-      int first, end;
-      block_at(*unit, item >> 1, first, end);
+      const int j = j_begin + (item >> 1);
+      const int first = j < blocks1 ? j * kBN : lo + (j - blocks1) * kBN, end = j < blocks1 ? sink_end : hi;
       const unsigned char* c = item & 1 ? p.planes.v_codes : p.planes.k_codes;
       const unsigned char* s = item & 1 ? p.planes.v_scales : p.planes.k_scales;
 #pragma unroll
@@ -266,6 +277,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid
       if (!unit->more) break;
       if (nblk > 0) {
         row0 = unit->row0;
+        j_begin = unit->j_begin;
+        blocks1 = unit->blocks1;
+        lo = unit->lo;
+        hi = unit->hi;
+        sink_end = unit->sink_end;
         load(0, 0);
         ok = queries(0) && (unit->ntile == 1 || queries(1));
 #pragma unroll 1
@@ -296,32 +312,20 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid
         if (lane == 0) give_unit(n);
         continue;
       }
-      const int nblk = u.nblk;
+      const int nblk = u.nblk, j_begin = u.j_begin, blocks1 = u.blocks1, lo = u.lo, hi = u.hi, sink_end = u.sink_end;
+      const int all_lo = u.all_lo, all_hi = u.all_hi, all_sink = u.all_sink;
       float m_used = kNoLogit, l = 0.f;
 #pragma unroll 1
       for (int j = 0; j < nblk; ++j) {
+        const int jj = j_begin + j;
+        const int first = jj < blocks1 ? jj * kBN : lo + (jj - blocks1) * kBN, end = jj < blocks1 ? sink_end : hi;
+        const bool hides = first + kBN > min(end, all_hi) || !(first >= all_lo || first + kBN <= all_sink);
         ok = bar_all(&bars->s_full[t], cnt & 1);
         if (!ok) break;
         tc_fence_after();
-        int first, end;
-        block_at(u, j, first, end);
-        if (__builtin_expect(first + kBN > min(end, u.all_hi) || !(first >= u.all_lo || first + kBN <= u.all_sink), 0)) {
-          // Hidden logits become -inf where they are, 32 rows at a time as bits.  (On all 128 in registers, with three comparisons
-          // for each, it took 4 us a block, and the code slowed down the blocks that do not run it.)
+        if (__builtin_expect(hides, 0)) {
           const int pos = u.len - u.nq + (u.m0 + t * kBM + row) / p.group;
-          const int hi = min(end, p.causal ? pos + 1 : end) - first;
-          const int lo = (p.window > 0 ? pos - p.window + 1 : 0) - first, sink = u.all_sink - first;
-#pragma unroll 1
-          for (int ch = 0; ch < 4; ++ch) {
-            const uint32_t keep = bits_below(hi - 32 * ch) & (~bits_below(lo - 32 * ch) | bits_below(sink - 32 * ch));
-            uint32_t z[32];
-            tmem_ld32(s_addr + ch * 32, z);
-            tmem_wait_ld();
-#pragma unroll
-            for (int i = 0; i < 32; ++i) z[i] = keep & (1u << i) ? z[i] : 0xff800000u;
-            tmem_st32(s_addr + ch * 32, z);
-          }
-          tmem_wait_st();
+          hide(s_addr, min(end, p.causal ? pos + 1 : end) - first, (p.window > 0 ? pos - p.window + 1 : 0) - first, all_sink - first);
         }
         uint32_t sr[kBN];
 #pragma unroll
