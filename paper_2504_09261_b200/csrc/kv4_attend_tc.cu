@@ -50,8 +50,11 @@ struct Unit {
   int b, kvh, head;                          // the stored head
   int len, nq, rows, m0, ntile;              // its length, tokens and query rows; first row and tiles of the unit (0: nothing to do)
   int tile, split;                           // number of its first tile in the head; share of the blocks
-  int blocks1, j_begin, nblk;                // blocks of the first run of rows, [0, sink_end); the unit's blocks
-  int lo, hi, sink_end, all_lo, all_hi, all_sink;   // Kv4Range
+  int j_begin, nblk;                         // its blocks
+  // The rows that its queries may see, [0, seam) and [seam + skip, seam + skip + ...), as one list of `total`: place v of it is row v, or
+  // v + skip from the seam on.  Blocks are 128 places.
+  int seam, skip, total;
+  int all_lo, all_hi, all_sink;              // Kv4Range
 };
 
 struct Bars {
@@ -81,7 +84,8 @@ __device__ __forceinline__ void make_unit(const Kv4AttendParams& p, int x, volat
   if (m0 >= rows) return;                    // queries of a padded batch that it does not have
   const int len = kv4_length(p, head, nq);
   const Kv4Range r = kv4_range(p, len, nq, m0, min(m0 + per * kBM, rows) - 1);
-  const uint32_t blocks = kv4_chunks(r, kBN), begin = blocks * split / p.splits;
+  const int total = r.sink_end + r.hi - r.lo;
+  const uint32_t blocks = (total + kBN - 1) / kBN, begin = blocks * split / p.splits;
   u.row0 = first_row(p.planes, head);
   u.b = b;
   u.kvh = head - b * p.kv_heads;
@@ -93,12 +97,11 @@ __device__ __forceinline__ void make_unit(const Kv4AttendParams& p, int x, volat
   u.ntile = per == 2 && m0 + kBM < rows ? 2 : 1;
   u.tile = tile;
   u.split = split;
-  u.blocks1 = (r.sink_end + kBN - 1) / kBN;
   u.j_begin = begin;
   u.nblk = blocks * (split + 1) / p.splits - begin;
-  u.lo = r.lo;
-  u.hi = r.hi;
-  u.sink_end = r.sink_end;
+  u.seam = r.sink_end;
+  u.skip = r.lo - r.sink_end;
+  u.total = total;
   u.all_lo = r.all_lo;
   u.all_hi = r.all_hi;
   u.all_sink = r.all_sink;
@@ -118,12 +121,14 @@ __device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity, Bars* b
   return true;
 }
 
-// Logits of a row that its query does not see become -inf where they are: columns from hi on, and those below lo from sink on.  32 at
-// a time, as bits.  (On all 128 in registers, with three comparisons for each, it took 4 us a block.)
-__device__ __forceinline__ void hide(uint32_t s_addr, int hi, int lo, int sink) {
+// Logits of places that a query does not see become -inf where they are.  It sees those below `head` (of the first run), and from the
+// seam on those below hi that are not below lo or are below sink.  32 at a time, as bits.  (On all 128 in registers, with three
+// comparisons for each, it took 4 us a block.)
+__device__ __forceinline__ void hide(uint32_t s_addr, int head, int seam, int hi, int lo, int sink) {
 #pragma unroll 1
   for (int ch = 0; ch < kBN / 32; ++ch) {
-    const uint32_t keep = bits_below(hi - 32 * ch) & (~bits_below(lo - 32 * ch) | bits_below(sink - 32 * ch));
+    const int at = 32 * ch;
+    const uint32_t keep = bits_below(head - at) | (bits_below(hi - at) & ~bits_below(seam - at) & (~bits_below(lo - at) | bits_below(sink - at)));
     if (__all_sync(0xffffffffu, keep == ~0u)) continue;
     uint32_t z[32];
     tmem_ld32(s_addr + ch * 32, z);
@@ -197,16 +202,16 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid
     uint32_t g = 0;                            // blocks of the units before
     const volatile Unit* unit = bars->unit;
     long long row0 = 0;
-    int j_begin = 0, blocks1 = 0, lo = 0, hi = 0, sink_end = 0;        // of the unit
+    int j_begin = 0, seam = 0, skip = 0, last = 0;        // of the unit
     auto load = [&](int item, int set) {       // item 2 j: keys of block j, 2 j + 1: its values
-      const int j = j_begin + (item >> 1);
-      const int first = j < blocks1 ? j * kBN : lo + (j - blocks1) * kBN, end = j < blocks1 ? sink_end : hi;
+      const int first = (j_begin + (item >> 1)) * kBN;
       const unsigned char* c = item & 1 ? p.planes.v_codes : p.planes.k_codes;
       const unsigned char* s = item & 1 ? p.planes.v_scales : p.planes.k_scales;
 #pragma unroll
       for (int i = 0; i < PASSES; ++i) {
-        // (a row past the end: any finite values, its logits do not count)
-        const long long row = row0 + min(first + i * 4 * RPW + row_in, end - 1);
+        // (a place past the end: any finite values, its logits do not count)
+        const int v = min(first + i * 4 * RPW + row_in, last);
+        const long long row = row0 + (v < seam ? v : v + skip);
         codes[set][i] = *reinterpret_cast<const uint4*>(c + row * (D / 2) + t * 16);
         scales[set][i] = *reinterpret_cast<const uint16_t*>(s + row * (D / 16) + t * 2);
       }
@@ -278,10 +283,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid
       if (nblk > 0) {
         row0 = unit->row0;
         j_begin = unit->j_begin;
-        blocks1 = unit->blocks1;
-        lo = unit->lo;
-        hi = unit->hi;
-        sink_end = unit->sink_end;
+        seam = unit->seam;
+        skip = unit->skip;
+        last = unit->total - 1;
         load(0, 0);
         ok = queries(0) && (unit->ntile == 1 || queries(1));
 #pragma unroll 1
@@ -312,20 +316,22 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid
         if (lane == 0) give_unit(n);
         continue;
       }
-      const int nblk = u.nblk, j_begin = u.j_begin, blocks1 = u.blocks1, lo = u.lo, hi = u.hi, sink_end = u.sink_end;
+      const int nblk = u.nblk, j_begin = u.j_begin, seam = u.seam, skip = u.skip, total = u.total;
       const int all_lo = u.all_lo, all_hi = u.all_hi, all_sink = u.all_sink;
       float m_used = kNoLogit, l = 0.f;
 #pragma unroll 1
       for (int j = 0; j < nblk; ++j) {
-        const int jj = j_begin + j;
-        const int first = jj < blocks1 ? jj * kBN : lo + (jj - blocks1) * kBN, end = jj < blocks1 ? sink_end : hi;
-        const bool hides = first + kBN > min(end, all_hi) || !(first >= all_lo || first + kBN <= all_sink);
+        const int first = (j_begin + j) * kBN, next = first + kBN;
+        // whether every query of the unit sees all of the block: up to its last row, and from its first row behind the seam on
+        const bool hides = next > total || (next > seam ? next + skip : next) > all_hi ||
+                           !(next <= seam || max(first, seam) + skip >= all_lo || next + skip <= all_sink);
         ok = bar_all(&bars->s_full[t], cnt & 1);
         if (!ok) break;
         tc_fence_after();
         if (__builtin_expect(hides, 0)) {
           const int pos = u.len - u.nq + (u.m0 + t * kBM + row) / p.group;
-          hide(s_addr, min(end, p.causal ? pos + 1 : end) - first, (p.window > 0 ? pos - p.window + 1 : 0) - first, all_sink - first);
+          const int hi = p.causal ? pos + 1 : u.len, lo = p.window > 0 ? pos - p.window + 1 : 0;
+          hide(s_addr, min(seam, hi) - first, seam - first, min(total, hi - skip) - first, lo - skip - first, all_sink - skip - first);
         }
         uint32_t sr[kBN];
 #pragma unroll
