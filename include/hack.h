@@ -422,7 +422,12 @@ typedef struct {
                                     limit of 1 makes the first wait that is not already satisfied give up */
   int64_t workspace_bytes;       /* size of the workspace given */
   hack_strides_t q, out;
+  int32_t form;                  /* 0: the library chooses its kernel by the sizes; HACK_KV4_FEW or HACK_KV4_MANY: that one, for
+                                    measurements and tests */
+  int32_t reserved;
 } hack_kv4_attend_t;
+enum { HACK_KV4_FEW = 1,         /* 8 or 16 query rows a CTA, any type */
+       HACK_KV4_MANY = 2 };      /* tiles of 128 query rows, bf16 */
 /* Device memory that a call of these sizes needs (it may be 0); it depends on the struct's sizes alone. */
 HACK_API hack_status_t hack_kv4_workspace(const hack_kv4_t* kv, const hack_kv4_attend_t* args, size_t* bytes);
 /* O = Softmax(sm_scale Q K^T) V over the stored rows that a query sees; a query that sees none gets zeros.  Logits,

@@ -27,6 +27,7 @@ RULE_FRACTION, RULE_RATIO = 0, 1
 HACK_ROPE_HALF, HACK_ROPE_PAIRS = 0, 1
 HACK_ROPE_PLAIN, HACK_ROPE_LINEAR, HACK_ROPE_BASE, HACK_ROPE_BANDS = 0, 1, 2, 3
 HACK_NORM_NONE, HACK_NORM_RMS, HACK_NORM_L2 = 0, 1, 2
+HACK_KV4_FEW, HACK_KV4_MANY = 1, 2
 
 EXPORTS = (
     "hack_split_budget", "hack_init_cache", "hack_free_cache", "hack_reset", "hack_set_obs_rows", "hack_get_limits",
@@ -95,7 +96,8 @@ class HackKv4Rows(C.Structure):
 
 class HackKv4Attend(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("dtype", "n_heads", "n_queries", "max_len", "appended", "causal", "window", "n_sink")] + [
-        ("sm_scale", C.c_float), ("wait_polls", C.c_int32), ("workspace_bytes", C.c_int64), ("q", HackStrides), ("out", HackStrides)]
+        ("sm_scale", C.c_float), ("wait_polls", C.c_int32), ("workspace_bytes", C.c_int64), ("q", HackStrides), ("out", HackStrides),
+        ("form", C.c_int32), ("reserved", C.c_int32)]
 
 
 class HackError(RuntimeError):
@@ -413,7 +415,7 @@ class HackKv4:
         if status:
             _check(status)
 
-    def _attend(self, q, out, lens, max_len, new_lens, appended, causal, n_sink, window, sm_scale, workspace_bytes):
+    def _attend(self, q, out, lens, max_len, new_lens, appended, causal, n_sink, window, sm_scale, workspace_bytes, form):
         self._lengths(lens, self.batch * self.n_kv_heads, "lens")
         self._lengths(new_lens, self.batch, "new_lens")
         _same("hack_kv4_attend", q, out)
@@ -421,22 +423,23 @@ class HackKv4:
                 q.get_device() != self.device:
             raise ValueError("q and out must be [batch, heads, tokens, head_dim] on the cache's device")
         return HackKv4Attend(_dtype_of(q), q.shape[1], q.shape[2], max_len, int(appended), int(causal), window, n_sink, sm_scale, 0,
-                             workspace_bytes, _strides_of(q, "q"), _strides_of(out, "out"))
+                             workspace_bytes, _strides_of(q, "q"), _strides_of(out, "out"), form, 0)
 
-    def hack_kv4_workspace(self, q, max_len: int, causal: bool = False, n_sink: int = 0, window: int = 0, appended: bool = False) -> int:
+    def hack_kv4_workspace(self, q, max_len: int, causal: bool = False, n_sink: int = 0, window: int = 0, appended: bool = False,
+                           form: int = 0) -> int:
         """Bytes of the workspace that hack_kv4_attend needs for queries of this shape and type."""
         need = C.c_size_t()
-        args = self._attend(q, q, None, max_len, None, appended, causal, n_sink, window, 0.0, 0)
+        args = self._attend(q, q, None, max_len, None, appended, causal, n_sink, window, 0.0, 0, form)
         _check(lib.hack_kv4_workspace(self._address, C.addressof(args), C.byref(need)))
         return need.value
 
     def hack_kv4_attend(self, q, out, lens, max_len: int, workspace=None, new_lens=None, appended: bool = False, causal: bool = False,
-                        n_sink: int = 0, window: int = 0, sm_scale: float = 0.0, stream=None) -> None:
+                        n_sink: int = 0, window: int = 0, sm_scale: float = 0.0, form: int = 0, stream=None) -> None:
         """q, out: [batch, heads, tokens, head_dim].  workspace: a uint8 tensor of hack_kv4_workspace bytes, or None where that
         is 0."""
         room = 0 if workspace is None else workspace.numel() * workspace.element_size()
-        args = _cached(self._key(max_len, appended, causal, n_sink, window, sm_scale, room, _key(q, out, lens, new_lens)),
-                       lambda: self._attend(q, out, lens, max_len, new_lens, appended, causal, n_sink, window, sm_scale, room))
+        args = _cached(self._key(max_len, appended, causal, n_sink, window, sm_scale, room, form, _key(q, out, lens, new_lens)),
+                       lambda: self._attend(q, out, lens, max_len, new_lens, appended, causal, n_sink, window, sm_scale, room, form))
         status = _invoke(_KV4_ATTEND, self._address, args, q, out, lens, new_lens, workspace if room else None, stream)
         if status:
             _check(status)

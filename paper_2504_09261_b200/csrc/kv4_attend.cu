@@ -12,8 +12,10 @@
 // empty as can be, and hold half the registers of the other way round.  Softmax with a running maximum that is
 // raised only when a logit exceeds it by 2^16; a CTA's warps are merged in shared memory, CTAs that share the rows of a head
 // (`splits`) through partial results in the workspace, which kv4_combine_kernel adds up.
-// fp32: queries and probabilities as sums of three bf16 numbers, which is all of their 24 bits.
-// kv4_attend_tc_kernel (kv4_attend_tc.cu): bf16, from kTcRows query rows on.
+// bf16: a probability is rounded once for the product with the values, which costs as much accuracy again as the rounding of the
+// result; as the sum of two bf16 numbers it costs a tenth of the time instead (32 heads of up to 65 536 rows 63 and 70 us).  fp32:
+// queries and probabilities as sums of three bf16 numbers, which is all of their 24 bits.
+// kv4_attend_tc_kernel (kv4_attend_tc.cu): bf16, many query rows.
 #include <algorithm>
 #include <cmath>
 #include <string>
@@ -35,7 +37,6 @@ constexpr int kCombineThreads = 256, kMaxSplits = 64;
 constexpr int kChunk = 32;                   // stored rows of a turn of a warp
 constexpr int kStages = 3;
 constexpr float kRaise = 16.f;               // log2 by which a logit may exceed the reference maximum
-constexpr int kTcRows = 48;                  // bf16: from so many query rows of a stored head on, tiles of 128 on the tensor cores
 constexpr uint32_t kWaitPolls = 1u << 24;    // of a wait in that kernel: a large part of a second at least
 
 template <int BYTES> __device__ __forceinline__ void cp_async(uint32_t dst, const void* src, int bytes) {
@@ -213,8 +214,12 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(F32, NQ)) kv4_attend_ker
     float s[NQ][2][4];
 #pragma unroll
     for (int T = 0; T < 2; ++T) {
+      float small[F32 ? NQ : 1][4];          // fp32: what the queries' second and third parts give
 #pragma unroll
-      for (int g = 0; g < NQ; ++g) s[g][T][0] = s[g][T][1] = s[g][T][2] = s[g][T][3] = 0.f;
+      for (int g = 0; g < NQ; ++g) {
+        s[g][T][0] = s[g][T][1] = s[g][T][2] = s[g][T][3] = 0.f;
+        if constexpr (F32) small[g][0] = small[g][1] = small[g][2] = small[g][3] = 0.f;
+      }
       uint32_t w[2][KS / 2];
       Scale2 sc[2][D / 64];
 #pragma unroll
@@ -245,13 +250,19 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(F32, NQ)) kv4_attend_ker
 #pragma unroll
               for (int k = NP - 1; k >= 0; --k) {
                 const uint2 q = q_smem[((k * NQ + g) * KS + 2 * x + u) * 32 + lane];
-                mma(s[g][T], a0, a1, a2, a3, q.x, q.y);
+                mma(k ? small[g] : s[g][T], a0, a1, a2, a3, q.x, q.y);
               }
             } else {
               mma(s[g][T], a0, a1, a2, a3, qf[g][2 * x + u].x, qf[g][2 * x + u].y);
             }
           }
         }
+      if constexpr (F32) {
+#pragma unroll
+        for (int g = 0; g < NQ; ++g)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[g][T][e] += small[g][e];
+      }
     }
     // ---- softmax
     if (first + kChunk > end || !kv4_all_see(p, range, first)) {
@@ -338,9 +349,20 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(F32, NQ)) kv4_attend_ker
           for (int i = 0; i < 2; ++i) {      // elements 8 x + 4 half + 2 i and + 1 of the lane's
             const uint32_t a0 = values2(w0, 8 * i, s0), a1 = values2(w0, 8 * i + 4, s0), a2 = values2(w1, 8 * i, s1), a3 = values2(w1, 8 * i + 4, s1);
 #pragma unroll
-            for (int g = 0; g < NQ; ++g)
+            for (int g = 0; g < NQ; ++g) {
+              float* const to = o[g][4 * x + 2 * half + i];
+              if constexpr (F32) {
+                // matrix instructions cut off what a sum does not hold: a long chain of them drifts by half a step each, so that
+                // fp32 adds their results to the outputs by itself
+                float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-              for (int k = NP - 1; k >= 0; --k) mma(o[g][4 * x + 2 * half + i], a0, a1, a2, a3, pf[k][g][T][0], pf[k][g][T][1]);
+                for (int k = NP - 1; k >= 0; --k) mma(sum, a0, a1, a2, a3, pf[k][g][T][0], pf[k][g][T][1]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) to[e] += sum[e];
+              } else {
+                mma(to, a0, a1, a2, a3, pf[0][g][T][0], pf[0][g][T][1]);
+              }
+            }
           }
         }
     }
@@ -499,6 +521,8 @@ hack_status_t check_attend(const hack_kv4_t* kv, const hack_kv4_attend_t* a) {
   if (a->n_heads < 1 || a->n_heads % kv->n_kv_heads) return invalid("n_heads must be a multiple of n_kv_heads");
   if (a->n_queries < 0 || a->max_len < 0) return invalid("n_queries and max_len must not be negative");
   if (a->window < 0 || a->n_sink < 0) return invalid("window and n_sink must not be negative");
+  if (a->form < 0 || a->form > HACK_KV4_MANY) return invalid("unknown form");
+  if (a->form == HACK_KV4_MANY && a->dtype != HACK_BF16) { set_error("HACK_KV4_MANY serves bf16"); return HACK_ERR_UNSUPPORTED; }
   if (a->wait_polls < 0) return invalid("wait_polls must not be negative");
   if (!(a->sm_scale >= 0.f) || !std::isfinite(a->sm_scale)) return invalid("sm_scale must be finite and non-negative");
   if ((long long)a->n_queries * (a->n_heads / kv->n_kv_heads) > 0x3fffffffll) return invalid("too many queries");
@@ -516,15 +540,24 @@ hack_status_t plan(const hack_kv4_t* kv, const hack_kv4_attend_t* a, Kv4AttendPa
   p.n_sink = a->window > 0 ? a->n_sink : 0;
   p.appended = a->appended != 0;
   const int heads = kv->batch * kv->n_kv_heads, rows = a->n_queries * p.group;
-  const bool tc = a->dtype == HACK_BF16 && rows >= kTcRows;
+  // rows that a tile of queries walks at most
+  long long walked = p.max_len;
+  if (p.window > 0) walked = std::min<long long>(walked, (long long)p.window + p.n_sink + p.n_queries);
+  // Which kernel: estimated us of a launch in one wave or more, fitted to both forms (us, few-rows form and tensor cores: 16 heads of
+  // 10 521 rows x 128, 32 queries 22.1 and 25.8, 48 26.8 and 26.6, 64 35.3 and 27.3; 64 heads of 2 240 rows, 48 queries 31.9 and 34.4,
+  // 64 38.9 and 35.9; 4 heads of 700 rows x 64, 64 queries 6.3 and 12.9; 128 heads of 680 rows 14.9 and 14.1).
+  const bool wide = kv->head_dim == 128;
+  // (16 heads, 1 024 queries: 64 and 128 rows 20.5 and 9.8 us: what a CTA costs at least)
+  const double few_tiles = (double)heads * ((rows + 15) / 16);
+  const double few_us = std::max(5.0 + (wide ? 1.45e-3 : 0.9e-3) * few_tiles * ((walked + 31) / 32),
+                                 8.0 * few_tiles / (sm_count() * ctas_per_sm(false, 2)));
+  const double tc_us = (wide ? 13.0 : 12.0) + (wide ? 10.7e-3 : 6.6e-3) * heads * ((rows + 127) / 128) * ((walked + 127) / 128);
+  const bool tc = a->form == 0 ? a->dtype == HACK_BF16 && rows > 16 && tc_us < few_us : a->form == HACK_KV4_MANY;
   p.tile_rows = tc ? 128 : rows <= 8 ? 8 : 16;
   p.tiles = (rows + p.tile_rows - 1) / p.tile_rows;
   const long long units = (long long)heads * p.tiles;
   if (units * p.tile_rows > 0x3fffffffll) { set_error("more query rows than a launch has places for"); return HACK_ERR_UNSUPPORTED; }
   p.units = (int)units;
-  // rows that a tile of queries walks at most
-  long long walked = p.max_len;
-  if (p.window > 0) walked = std::min<long long>(walked, (long long)p.window + p.n_sink + p.n_queries);
   const int sms = sm_count();
   if (tc) {
     p.tiles_per_cta = units <= sms ? 1 : 2;

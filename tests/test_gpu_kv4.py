@@ -135,7 +135,7 @@ def test_append_strided_padded_and_full(hb):
 
 # ------------------------------------------------------------------ attention
 def _check(hb, g, dtype, dim, batch, kv_heads, group, tokens, cap, lens, max_len=None, causal=False, window=0, n_sink=0, new_lens=None,
-           appended=False, sm_scale=0.0, row_off=None, rows=None, q_layout="token", q_size=1.0, planes=None, random_planes=True):
+           appended=False, sm_scale=0.0, row_off=None, rows=None, q_layout="token", q_size=1.0, planes=None, form=0):
     rows = rows or batch * kv_heads * cap
     if planes is None:
         planes = Planes(rows, dim)
@@ -148,10 +148,10 @@ def _check(hb, g, dtype, dim, batch, kv_heads, group, tokens, cap, lens, max_len
     max_len = cap if max_len is None else max_len
     lens_dev = _ints(*lens)
     new_dev = None if new_lens is None else _ints(*new_lens)
-    need = kv4.hack_kv4_workspace(q, max_len, causal=causal, n_sink=n_sink, window=window, appended=appended)
+    need = kv4.hack_kv4_workspace(q, max_len, causal=causal, n_sink=n_sink, window=window, appended=appended, form=form)
     work = torch.full((need + 64,), 0xff, dtype=torch.uint8, device="cuda")          # NaN for whoever reads what nobody wrote
     call = lambda: kv4.hack_kv4_attend(q, out, lens_dev, max_len, workspace=work[:need], new_lens=new_dev, appended=appended,   # noqa: E731
-                                       causal=causal, n_sink=n_sink, window=window, sm_scale=sm_scale)
+                                       causal=causal, n_sink=n_sink, window=window, sm_scale=sm_scale, form=form)
     call()
     first = out.clone()
     call()
@@ -325,35 +325,47 @@ MANY = [  # dim, batch, kv_heads, group, tokens, cap
 
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("dim,batch,kv_heads,group,tokens,cap", MANY)
-def test_attend_many_queries(hb, causal, dim, batch, kv_heads, group, tokens, cap):
+@pytest.mark.parametrize("form", [1, 2])
+def test_attend_many_queries(hb, form, causal, dim, batch, kv_heads, group, tokens, cap):
     n = batch * kv_heads
     lens = [cap] + [(i * 101) % (cap + 1) for i in range(1, n)]
-    _check(hb, _gen(cap), torch.bfloat16, dim, batch, kv_heads, group, tokens, cap, lens, causal=causal)
+    _check(hb, _gen(cap), torch.bfloat16, dim, batch, kv_heads, group, tokens, cap, lens, causal=causal, form=form)
 
 
 @pytest.mark.parametrize("length", [0, 1, 31, 32, 33, 127, 128, 129, 255, 256, 257, 384, 511])
 @pytest.mark.parametrize("dim", [64, 128])
 def test_attend_many_queries_lengths(hb, dim, length):
-    _check(hb, _gen(length), torch.bfloat16, dim, 1, 2, 1, 140, 512, [length, 512 - length], causal=dim == 64)
-    _check(hb, _gen(length), torch.bfloat16, dim, 1, 2, 3, 100, 512, [length, 512 - length], causal=dim == 128)
+    _check(hb, _gen(length), torch.bfloat16, dim, 1, 2, 1, 140, 512, [length, 512 - length], causal=dim == 64, form=2)
+    _check(hb, _gen(length), torch.bfloat16, dim, 1, 2, 3, 100, 512, [length, 512 - length], causal=dim == 128, form=2)
 
 
 @pytest.mark.parametrize("tokens", [60, 200])
 @pytest.mark.parametrize("window,n_sink", [(1, 0), (1, 1), (7, 4), (128, 0), (100, 140), (300, 3), (1000, 5)])
 @pytest.mark.parametrize("causal", [True, False])
 def test_attend_many_queries_window(hb, tokens, window, n_sink, causal):
-    _check(hb, _gen(window), torch.bfloat16, 64, 1, 3, 2, tokens, 700, [700, 190, 12], causal=causal, window=window, n_sink=n_sink)
-    _check(hb, _gen(window), torch.bfloat16, 128, 1, 1, 1, tokens, 700, [611], causal=causal, window=window, n_sink=n_sink)
+    _check(hb, _gen(window), torch.bfloat16, 64, 1, 3, 2, tokens, 700, [700, 190, 12], causal=causal, window=window, n_sink=n_sink, form=2)
+    _check(hb, _gen(window), torch.bfloat16, 128, 1, 1, 1, tokens, 700, [611], causal=causal, window=window, n_sink=n_sink, form=2)
 
 
 def test_attend_many_queries_padded_and_limits(hb):
     g, dt = _gen(22), torch.bfloat16
-    _check(hb, g, dt, 128, 3, 2, 2, 150, 400, [10, 94, 50, 99, 0, 7], new_lens=[150, 70, 0], appended=True, causal=True)
-    _check(hb, g, dt, 64, 2, 2, 1, 300, 500, [-3, 2 ** 31 - 1, 50, 0], new_lens=[-1, 900], appended=True, causal=True)
-    _check(hb, g, dt, 64, 2, 2, 1, 64, 500, [2 ** 31 - 1, -2 ** 31, 49, 1], max_len=300)
-    _check(hb, g, dt, 64, 1, 1, 1, 64, 50, [20], max_len=0)
-    _check(hb, g, dt, 128, 1, 3, 1, 70, 140, [140, 3, 121], row_off=torch.tensor([281, 0, 140], dtype=torch.int64, device="cuda"), rows=422, q_layout="head")
-    _check(hb, g, dt, 128, 1, 3, 1, 70, 140, [140, 3, 21], sm_scale=2.5, q_size=3.0)
+    kw = dict(form=2)
+    _check(hb, g, dt, 128, 3, 2, 2, 150, 400, [10, 94, 50, 99, 0, 7], new_lens=[150, 70, 0], appended=True, causal=True, **kw)
+    _check(hb, g, dt, 64, 2, 2, 1, 300, 500, [-3, 2 ** 31 - 1, 50, 0], new_lens=[-1, 900], appended=True, causal=True, **kw)
+    _check(hb, g, dt, 64, 2, 2, 1, 64, 500, [2 ** 31 - 1, -2 ** 31, 49, 1], max_len=300, **kw)
+    _check(hb, g, dt, 64, 1, 1, 1, 64, 50, [20], max_len=0, **kw)
+    _check(hb, g, dt, 128, 1, 3, 1, 70, 140, [140, 3, 121], row_off=torch.tensor([281, 0, 140], dtype=torch.int64, device="cuda"), rows=422, q_layout="head", **kw)
+    _check(hb, g, dt, 128, 1, 3, 1, 70, 140, [140, 3, 21], sm_scale=2.5, q_size=3.0, **kw)
+
+
+def test_the_library_chooses(hb):
+    """Both forms' workspaces are those of the library's own choice, one way or the other, at sizes timed in both."""
+    for dim, heads, tokens, cap, many in ((128, 16, 32, 10521, False), (128, 16, 64, 10521, True), (128, 64, 64, 2240, True),
+                                          (64, 4, 64, 700, False), (128, 16, 1024, 64, True), (64, 256, 256, 680, True)):
+        kv4 = Planes(heads * cap, dim).handle(hb, 1, heads, cap)
+        q = torch.empty(1, heads, tokens, dim, dtype=torch.bfloat16, device="cuda")
+        need = [kv4.hack_kv4_workspace(q, cap, form=f) for f in range(3)]
+        assert need[0] == need[2 if many else 1], (dim, heads, tokens, cap, need)
 
 
 def test_rows_whose_output_starts_on_16_bytes_only(hb):
@@ -364,7 +376,13 @@ def test_rows_whose_output_starts_on_16_bytes_only(hb):
     kv4 = planes.handle(hb, 1, 1, cap)
     wide = torch.full((1, 1, n, dim + 8), 5.0, dtype=torch.bfloat16, device="cuda")
     q = torch.randn(1, 1, n, dim + 8, generator=g, device="cuda").to(torch.bfloat16)[..., 8:]
-    kv4.hack_kv4_attend(q, wide[..., 8:], _ints(cap), cap, workspace=torch.empty(1 << 24, dtype=torch.uint8, device="cuda"))
+    for form in (1, 2):
+        wide.fill_(5.0)
+        kv4.hack_kv4_attend(q, wide[..., 8:], _ints(cap), cap, workspace=torch.empty(1 << 24, dtype=torch.uint8, device="cuda"), form=form)
+        _rows_on_16_bytes(planes, q, wide, cap, n, dim)
+
+
+def _rows_on_16_bytes(planes, q, wide, cap, n, dim):
     want = ref.attend(q[0], ref.values(planes.k_codes, planes.k_scales), ref.values(planes.v_codes, planes.v_scales), cap, n, dim ** -0.5)
     assert ((wide[0, ..., 8:].double() - want[0]).abs() <= ref.bound(*want, torch.bfloat16, dim, cap)).all()
     assert (wide[..., :8] == 5.0).all()
@@ -381,18 +399,18 @@ def test_a_wait_that_runs_out_is_reported(hb, dim):
     q = torch.randn(1, 2, n, dim, generator=g, device="cuda").to(torch.bfloat16)
     out, good = torch.empty_like(q), torch.empty_like(q)
     lens = _ints(cap, cap)
-    need = kv4.hack_kv4_workspace(q, cap)
+    need = kv4.hack_kv4_workspace(q, cap, form=hb.HACK_KV4_MANY)
     work = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
-    kv4.hack_kv4_attend(q, good, lens, cap, workspace=work)
+    kv4.hack_kv4_attend(q, good, lens, cap, workspace=work, form=hb.HACK_KV4_MANY)
     kv4.hack_kv4_poll_status()
-    args = kv4._attend(q, out, lens, cap, None, False, False, 0, 0, 0.0, work.numel())
+    args = kv4._attend(q, out, lens, cap, None, False, False, 0, 0, 0.0, work.numel(), hb.HACK_KV4_MANY)
     args.wait_polls = 1
     assert bd.lib.hack_kv4_attend(kv4._address, C.addressof(args), q.data_ptr(), out.data_ptr(), lens.data_ptr(), None, work.data_ptr(), None) == 0
     with pytest.raises(hb.HackError) as e:
         kv4.hack_kv4_poll_status()
     assert e.value.status == 6
     kv4.hack_kv4_poll_status()                                    # reported once
-    kv4.hack_kv4_attend(q, out, lens, cap, workspace=work)        # and the next call is right
+    kv4.hack_kv4_attend(q, out, lens, cap, workspace=work, form=hb.HACK_KV4_MANY)        # and the next call is right
     assert torch.equal(out, good)
     kv4.hack_kv4_poll_status()
 

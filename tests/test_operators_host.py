@@ -123,12 +123,13 @@ def test_kv4_rows_refused(hb, change, status):
 
 @pytest.mark.parametrize("change,status", [
     (dict(dtype=3), 2), (dict(n_heads=4), 1), (dict(n_heads=0), 1), (dict(n_queries=-1), 1), (dict(max_len=-1), 1), (dict(window=-1), 1),
-    (dict(n_sink=-1), 1), (dict(sm_scale=-1.0), 1), (dict(sm_scale=float("nan")), 1), (dict(n_queries=1 << 30), 1), (dict(wait_polls=-1), 1)])
+    (dict(n_sink=-1), 1), (dict(sm_scale=-1.0), 1), (dict(sm_scale=float("nan")), 1), (dict(n_queries=1 << 30), 1), (dict(wait_polls=-1), 1), (dict(form=3), 1),
+    (dict(form=2, dtype=0), 2)])
 def test_kv4_attend_refused(hb, change, status):
     from paper_2504_09261_b200 import binding as bd
     f = dict(dtype=1, n_heads=6, n_queries=1, max_len=10, appended=0, causal=0, window=0, n_sink=0, sm_scale=0.0, wait_polls=0, workspace_bytes=0)
-    f.update(change)
-    args = bd.HackKv4Attend(*f.values(), bd.HackStrides(768, 128, 128), bd.HackStrides(768, 128, 128))
+    f.update({k: v for k, v in change.items() if k in f})
+    args = bd.HackKv4Attend(*f.values(), bd.HackStrides(768, 128, 128), bd.HackStrides(768, 128, 128), change.get("form", 0), 0)
     kv = _kv4()
     k, a, need = C.addressof(kv), C.addressof(args), C.c_size_t()
     assert bd.lib.hack_kv4_workspace(k, a, C.byref(need)) == status
