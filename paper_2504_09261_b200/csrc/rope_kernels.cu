@@ -20,7 +20,7 @@
 namespace hack {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 constexpr int kUnroll = 4;          // rows of a group in flight
 
 struct RopeParams {
@@ -37,7 +37,7 @@ struct RopeParams {
   int tile_tokens;                  // tokens of a CTA, a power of two no larger than its groups
   int chunk_heads;                  // heads of a CTA
   int norm;
-  float eps;
+  float eps, inv_eps;
   const void* positions;
   int positions_f32;
   long long positions_stride;
@@ -79,7 +79,7 @@ template <> struct Vec<__nv_bfloat16> {
 
 // LANED: in the half layout, a lane's elements have their partners in one other lane (rotary_dim / 2 a multiple of them).
 template <typename T, int D, bool LANED>
-__global__ void __launch_bounds__(kThreads, 4) rope_kernel(const __grid_constant__ RopeParams p) {
+__global__ void __launch_bounds__(kThreads, 6) rope_kernel(const __grid_constant__ RopeParams p) {
   constexpr int N = Vec<T>::N, LANES = D / N, GROUPS = kThreads / LANES;
   extern __shared__ float2 cs[];                       // [tile_tokens][pairs] cosine, sine
   __shared__ float staged[LANED ? 1 : GROUPS][LANED ? 1 : D + 4];   // whole rows, where partners are anywhere
@@ -165,26 +165,39 @@ __global__ void __launch_bounds__(kThreads, 4) rope_kernel(const __grid_constant
   // what neither turns nor is scaled leaves as it came
   const bool as_is = p.norm == HACK_NORM_NONE && !weight && !gain && (!rotate || e0 >= 2 * half);
 
-  // all groups of a warp take the same number of turns: the shuffles need every lane
+  // All groups of a warp take the same number of turns: the shuffles need every lane.  The rows in flight go through each
+  // step together (row by row, a chain of shuffles each, the bf16 form took 89 us where this takes less).
   for (int h0 = h_first; h0 < h_end; h0 += head_lanes * kUnroll) {
     if (h0 > h_first) load(h0);
+    float f[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int h = h0 + u * head_lanes + head_of;
-      if (h0 + u * head_lanes >= h_end) break;         // the same for the whole CTA
-      const bool mine = live && h < h_end;
-      float x[N];
-      Vec<T>::unpack(raw[u], x);
-      float f = mine && gain ? gain[h] : 1.f;
-      if (p.norm != HACK_NORM_NONE) {
-        float sum = 0.f;
+      f[u] = gain && h < h_end ? gain[h] : 1.f;
+    }
+    if (p.norm != HACK_NORM_NONE) {
+      float sum[kUnroll];
 #pragma unroll
-        for (int e = 0; e < N; ++e) sum = fmaf(x[e], x[e], sum);
+      for (int u = 0; u < kUnroll; ++u) {
+        float x[N];
+        Vec<T>::unpack(raw[u], x);
+        sum[u] = 0.f;
 #pragma unroll
-        for (int o = LANES / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o, LANES);
-        f *= p.norm == HACK_NORM_RMS ? 1.f / sqrtf(sum * (1.f / D) + p.eps) : 1.f / fmaxf(sqrtf(sum), p.eps);
+        for (int e = 0; e < N; ++e) sum[u] = fmaf(x[e], x[e], sum[u]);
       }
-      float y[N];
+#pragma unroll
+      for (int o = LANES / 2; o > 0; o >>= 1)
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) sum[u] += __shfl_xor_sync(0xffffffffu, sum[u], o, LANES);
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u)
+        f[u] *= p.norm == HACK_NORM_RMS ? rsqrtf(fmaf(sum[u], 1.f / D, p.eps)) : fminf(rsqrtf(sum[u]), p.inv_eps);
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int h = h0 + u * head_lanes + head_of;
+      float x[N], y[N];
+      Vec<T>::unpack(raw[u], x);
       if (rotate) {
         float xp[N];                                   // the partners
         if (!halves) {
@@ -212,13 +225,13 @@ __global__ void __launch_bounds__(kThreads, 4) rope_kernel(const __grid_constant
         // (an element that does not turn has factor 0 for a partner that may be infinite)
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-          y[e] = f * (e0 + e < 2 * half ? fmaf(x[e], own[e], xp[e] * other[e]) : x[e] * own[e]);
+          y[e] = f[u] * (e0 + e < 2 * half ? fmaf(x[e], own[e], xp[e] * other[e]) : x[e] * own[e]);
         }
       } else {
 #pragma unroll
-        for (int e = 0; e < N; ++e) y[e] = x[e] * (f * own[e]);
+        for (int e = 0; e < N; ++e) y[e] = x[e] * (f[u] * own[e]);
       }
-      if (mine) *reinterpret_cast<uint4*>(out + h * out_head) = as_is ? raw[u] : Vec<T>::pack(y);
+      if (live && h < h_end) *reinterpret_cast<uint4*>(out + h * out_head) = as_is ? raw[u] : Vec<T>::pack(y);
     }
   }
 }
@@ -229,8 +242,8 @@ int launch(RopeParams& p, cudaStream_t st) {
   p.tile_tokens = 1;
   while (p.tile_tokens < GROUPS && p.tile_tokens < p.n_tokens) p.tile_tokens *= 2;
   p.tiles = (p.n_tokens + p.tile_tokens - 1) / p.tile_tokens;
-  // Heads of a CTA: as many as leave four CTAs for every SM, so that cosines, weights and the launch of a CTA are shared,
-  // but no more than four turns.
+  // Heads of a CTA: as many as leave two CTAs for every SM, so that cosines, weights and the launch of a CTA are shared,
+  // but no more than eight turns (four: 85 us where eight take 77, sixteen 77).
   const int head_lanes = GROUPS / p.tile_tokens, most = std::max({p.heads[0], p.heads[1], p.heads[2]});
   p.chunk_heads = head_lanes;
   auto count = [&](int per) {
@@ -238,7 +251,7 @@ int launch(RopeParams& p, cudaStream_t st) {
     for (int k = 0; k < 3; ++k) n += (p.heads[k] + per - 1) / per;
     return n * p.tiles * p.batch;
   };
-  while (p.chunk_heads < most && p.chunk_heads < 4 * kUnroll * head_lanes && count(2 * p.chunk_heads) >= 4ll * sm_count()) p.chunk_heads *= 2;
+  while (p.chunk_heads < most && p.chunk_heads < 8 * kUnroll * head_lanes && count(2 * p.chunk_heads) >= 2ll * sm_count()) p.chunk_heads *= 2;
   const long long grid = count(p.chunk_heads);
   if (grid > 0x7fffffffll) {
     set_error("rotation: more rows than a launch has places for");
@@ -420,6 +433,7 @@ extern "C" hack_status_t hack_qk_norm_rope(const hack_rope_plan_t* plan, const h
   p.n_tokens = a.n_tokens;
   p.norm = a.norm;
   p.eps = a.eps;
+  p.inv_eps = 1.f / a.eps;
   if (plan) set_rotation(p, plan, positions, a.positions_f32 != 0, a.positions_stride, false);
   return done(launch_any(p, a.dtype, a.head_dim, (cudaStream_t)stream));
 }
