@@ -2,10 +2,9 @@
 //
 // A thread owns a block of 16 elements of K and the same block of V: 32 (bf16) or 64 (fp32) bytes in, eight bytes of codes and
 // one of scale out, so that a warp reads and writes consecutive bytes, and nothing is exchanged.  Bound: bytes, if the
-// arithmetic stays under them: about a dozen instructions an element in (largest of a block on the bits; one FMA that
-// rounds into the low bits of a number, and one that shows whether it fell on the wrong side, as the reciprocal is inexact),
-// two an element out (codes to bf16 as in the attention; a conversion of integers an element took 30 us of the special-function
-// unit's time where the bytes take 26).
+// arithmetic stays under them: five instructions an element in for bf16 (largest of a block on the bits, a quotient
+// rounded into the low bits of a number), about a dozen for fp32, two an element out (codes to bf16 as in the
+// attention; a conversion of integers an element took 30 us of the special-function unit's time where the bytes take 26).
 #include <string>
 
 #include "entry_checks.h"
@@ -63,6 +62,10 @@ template <> struct Sixteen<float> {
     for (int i = 0; i < 16; ++i) m = max(m, w[i] & 0x7fffffffu);
     return m;
   }
+  __device__ __forceinline__ void limit(float most) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(fminf(fmaxf(at(i), -most), most));
+  }
   __device__ __forceinline__ void no_nans() {
 #pragma unroll
     for (int i = 0; i < 16; ++i)
@@ -78,6 +81,14 @@ template <> struct Sixteen<__nv_bfloat16> {
 #pragma unroll
     for (int i = 0; i < 8; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
     return max(m & 0xffff0000u, m << 16);
+  }
+  // (seven times the largest scale is a bf16 number)
+  __device__ __forceinline__ void limit(float most) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float x = fminf(fmaxf(at(2 * i), -most), most), y = fminf(fmaxf(at(2 * i + 1), -most), most);
+      w[i] = __float_as_uint(x) >> 16 | (__float_as_uint(y) & 0xffff0000u);
+    }
   }
   __device__ __forceinline__ void no_nans() {
 #pragma unroll
@@ -102,23 +113,32 @@ template <typename T> __device__ __forceinline__ uint2 quantise(Sixteen<T>& x, u
   if (e < 255 && 7.f * scale_value(e) < top) ++e;
   if (e > 0 && 7.f * scale_value(e - 1) >= top) --e;
   byte = e;
-  const float s = scale_value(e), inv = 1.f / s, most = 7.f * s;
-  const int half = __float_as_int(0.5f * s);
-  const bool beyond = top > most;              // the largest scale of all: what lies beyond seven of it is limited
-  // x inv + kMagic has c + 8 in its low bits.  The inexact inv may put it on the wrong side of the middle between two
-  // codes, or off it: what is left of x beside the code, which is exact, tells.
+  const float s = scale_value(e), inv = 1.f / s;
+  if (top > 7.f * s) x.limit(7.f * s);         // the largest scale of all, and beyond seven of it
+  // A quotient + kMagic has c + 8 in its low bits, ties to even.
   constexpr float kMagic = 12582912.f + 8.f;
   uint32_t code[2] = {0, 0};
+  if constexpr (sizeof(T) == 2) {
+    // x (inv + rest) is within 2^-48 of x / s, so that its product is the quotient correctly rounded: exactly the middle between two
+    // codes where x / s is (eight significant bits over four do not come nearer to one without being it).
+    const float rest = fmaf(-s, inv, 1.f) * inv;
 #pragma unroll
-  for (int i = 0; i < kBlock; ++i) {
-    float v = x.at(i);
-    if (beyond) v = fminf(fmaxf(v, -most), most);
-    const float r = fmaf(v, inv, kMagic);
-    int n = __float_as_int(r);
-    const float left = fmaf(kMagic - r, s, v);
-    // on the middle, an odd code gives way: the float below one half of s
-    if (fabsf(left) > __int_as_float(half - (n & 1))) n += (__float_as_int(left) >> 31) | 1;
-    code[i >> 3] += (uint32_t)n << (4 * (i & 7));
+    for (int i = 0; i < kBlock; ++i) {
+      const float v = x.at(i);
+      code[i >> 3] += __float_as_uint(fmaf(v, inv, v * rest) + kMagic) << (4 * (i & 7));
+    }
+  } else {
+    // The quotient may fall on the wrong side of a middle, or on it: what is left of x beside the code, which is exact, tells.
+    const int half = __float_as_int(0.5f * s);
+#pragma unroll
+    for (int i = 0; i < kBlock; ++i) {
+      const float v = x.at(i), r = fmaf(v, inv, kMagic);
+      int n = __float_as_int(r);
+      const float left = fmaf(kMagic - r, s, v);
+      // on the middle, an odd code gives way: the float below one half of s
+      if (fabsf(left) > __int_as_float(half - (n & 1))) n += (__float_as_int(left) >> 31) | 1;
+      code[i >> 3] += (uint32_t)n << (4 * (i & 7));
+    }
   }
   // (the bits of kMagic without its 8, once for each of the eight codes)
   constexpr uint32_t kBase = 0x4b400000u;
