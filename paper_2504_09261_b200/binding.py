@@ -282,13 +282,14 @@ _args_of = {}     # argument structs by shapes, strides and types: they hold not
 
 
 def _cached(key, make):
+    """(struct, its address); the caller holds on to it for the call, as another thread may empty the store."""
     args = _args_of.get(key)
     if args is None:
         if len(_args_of) >= 4096:
             _args_of.clear()
         made = make()
         args = _args_of[key] = (made, C.addressof(made))
-    return args[1]
+    return args
 
 
 def hack_rope_plan(head_dim: int, rotary_dim: Optional[int] = None, layout: int = HACK_ROPE_HALF, axes: int = 1,
@@ -315,7 +316,7 @@ def hack_rope(plan: HackRopePlan, x, y, positions, transpose: bool = False, stre
                             _strides_of(y, "y"))
 
     args = _cached((axes, plan.head_dim, transpose, _key(x, y, positions)), make)
-    status = _invoke(_ROPE, C.addressof(plan), args, x, y, positions, stream)
+    status = _invoke(_ROPE, C.addressof(plan), args[1], x, y, positions, stream)
     if status:
         _check(status)
 
@@ -348,7 +349,7 @@ def hack_qk_norm_rope(plan: Optional[HackRopePlan], q, k, v, q_out, k_out, v_out
     args = _cached((None if plan is None else (plan.axes, plan.head_dim), norm, eps,
                     _key(q, k, v, q_out, k_out, v_out, positions, q_weight, k_weight, q_gain, k_gain)),
                    lambda: _qkv_args(plan, q, k, v, q_out, k_out, v_out, positions, norm, eps, q_weight, k_weight, q_gain, k_gain))
-    status = _invoke(_QK_NORM_ROPE, None if plan is None else C.addressof(plan), args, q, k, v, q_out, k_out, v_out, positions,
+    status = _invoke(_QK_NORM_ROPE, None if plan is None else C.addressof(plan), args[1], q, k, v, q_out, k_out, v_out, positions,
                      q_weight, k_weight, q_gain, k_gain, stream)
     if status:
         _check(status)
@@ -405,13 +406,13 @@ class HackKv4:
 
     def hack_kv4_append(self, k, v, lens, new_lens=None, stream=None) -> None:
         args = _cached(self._key("rows", _key(k, v, lens, new_lens)), lambda: self._rows(k, v, lens, new_lens))
-        status = _invoke(_KV4_APPEND, self._address, args, k, v, lens, new_lens, stream)
+        status = _invoke(_KV4_APPEND, self._address, args[1], k, v, lens, new_lens, stream)
         if status:
             _check(status)
 
     def hack_kv4_read(self, k_out, v_out, first, stream=None) -> None:
         args = _cached(self._key("rows", _key(k_out, v_out, first, None)), lambda: self._rows(k_out, v_out, first, None))
-        status = _invoke(_KV4_READ, self._address, args, k_out, v_out, first, stream)
+        status = _invoke(_KV4_READ, self._address, args[1], k_out, v_out, first, stream)
         if status:
             _check(status)
 
@@ -440,7 +441,7 @@ class HackKv4:
         room = 0 if workspace is None else workspace.numel() * workspace.element_size()
         args = _cached(self._key(max_len, appended, causal, n_sink, window, sm_scale, room, form, _key(q, out, lens, new_lens)),
                        lambda: self._attend(q, out, lens, max_len, new_lens, appended, causal, n_sink, window, sm_scale, room, form))
-        status = _invoke(_KV4_ATTEND, self._address, args, q, out, lens, new_lens, workspace if room else None, stream)
+        status = _invoke(_KV4_ATTEND, self._address, args[1], q, out, lens, new_lens, workspace if room else None, stream)
         if status:
             _check(status)
 
@@ -543,7 +544,7 @@ class HackCache:
         args = _cached((None if plan is None else (plan.axes, plan.head_dim), norm, eps, "step",
                         _key(q, k, v, positions, q_weight, k_weight, q_gain, k_gain)),
                        lambda: _qkv_args(plan, q, k, v, q, k, v, positions, norm, eps, q_weight, k_weight, q_gain, k_gain))
-        _check(lib.hack_scale_step_qkv(self._h, layer, scale, None if plan is None else C.addressof(plan), args, _ptr(q), _ptr(k),
+        _check(lib.hack_scale_step_qkv(self._h, layer, scale, None if plan is None else C.addressof(plan), args[1], _ptr(q), _ptr(k),
                                        _ptr(v), _ptr(positions), _ptr(q_weight), _ptr(k_weight), _ptr(q_gain), _ptr(k_gain), _ptr(out),
                                        _ptr(stream)))
 

@@ -536,8 +536,9 @@ hack_status_t plan(const hack_kv4_t* kv, const hack_kv4_attend_t* a, Kv4AttendPa
   p.n_queries = a->n_queries;
   p.max_len = std::min(a->max_len, kv->cap);
   p.causal = a->causal != 0;
-  p.window = a->window;
-  p.n_sink = a->window > 0 ? a->n_sink : 0;
+  // (positions are above -2^30: a window or a number of first rows that reaches past all of them must not wrap)
+  p.window = std::min(a->window, 1 << 30);
+  p.n_sink = a->window > 0 ? std::min(a->n_sink, 1 << 30) : 0;
   p.appended = a->appended != 0;
   const int heads = kv->batch * kv->n_kv_heads, rows = a->n_queries * p.group;
   // rows that a tile of queries walks at most

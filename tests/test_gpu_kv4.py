@@ -215,6 +215,12 @@ def test_attend_padded_batch_and_limits(hb, dtype):
     _check(hb, g, dtype, 128, 1, 3, 1, 2, 40, [40, 3, 21], sm_scale=2.5, q_size=3.0)
 
 
+@pytest.mark.parametrize("dtype,form", [(torch.float32, 0), (torch.bfloat16, 1), (torch.bfloat16, 2)])
+def test_attend_windows_past_every_position(hb, dtype, form):
+    for window, n_sink in ((2 ** 31 - 1, 0), (2 ** 31 - 1, 2 ** 31 - 1), (5, 2 ** 31 - 1)):
+        _check(hb, _gen(30), dtype, 64, 1, 2, 1, 60, 200, [200, 30], causal=True, window=window, n_sink=n_sink, form=form)
+
+
 def test_attend_equal_and_dominant_logits(hb):
     """All logits equal: the mean of the values.  One far above the others: that value, although the maximum comes last."""
     dim, cap = 64, 500
@@ -469,6 +475,51 @@ def test_from_projections_to_a_stored_cache(hb, config):
         assert ((out[i // h, i % h].double() - want[0][0]).abs() <= ref.bound(*want, dt, d, n)[0]).all()
     one.close()
     two.close()
+
+
+def test_decode_from_projections_in_a_graph(hb):
+    """A whole decode that starts from projections, captured after the call that makes the buffers, replayed with other inputs."""
+    from tests.parity_util import make_cache
+    from workloads import SyntheticQKV, get_config
+    cfg = get_config(1, n_layers=2)
+    cache = make_cache(cfg, SyntheticQKV(cfg).head_is_contextual.numpy())
+    b, h, d = cfg.batch, cfg.n_heads, cfg.head_dim
+    g = _gen(41)
+    plan = hb.hack_rope_plan(d, d // 2, layout=hb.HACK_ROPE_PAIRS)
+    data = []
+    for side in cfg.sides:
+        n = side * side
+        qkv = [torch.randn(b, n, 3, h, d, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2)]
+        data.append((qkv, [torch.empty(b, h, n, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)],
+                     torch.arange(n, dtype=torch.int32, device="cuda")))
+
+    def loop(stream):
+        cache.hack_reset()
+        for scale, (qkv, outs, pos) in enumerate(data):
+            for layer in range(2):
+                cache.hack_scale_step_qkv(layer, scale, plan, *(qkv[layer][:, :, i].transpose(1, 2) for i in range(3)), outs[layer], pos,
+                                          stream=stream)
+
+    loop(None)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        loop(torch.cuda.current_stream().cuda_stream)
+    for qkv, _, _ in data:
+        for x in qkv:
+            x.copy_(torch.randn(x.shape, generator=g, device="cuda"))
+    loop(None)
+    torch.cuda.synchronize()
+    want = [[o.clone() for o in outs] for _, outs, _ in data]
+    for _, outs, _ in data:
+        for o in outs:
+            o.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    for w, (_, outs, _) in zip(want, data):
+        assert torch.equal(w[0], outs[0]) and torch.equal(w[1], outs[1])
+    cache.hack_poll_status()
+    cache.close()
 
 
 def test_step_from_projections_refuses(hb):
