@@ -140,6 +140,29 @@ __device__ __forceinline__ void hide(uint32_t s_addr, int head, int seam, int hi
   tmem_wait_st();
 }
 
+// A row of a tile of queries into shared memory, elements in the order 0 4 1 5 2 6 3 7 of every eight.
+template <int D>
+__device__ __forceinline__ void load_queries(const Kv4AttendParams& p, const volatile Unit& u, int tile, int row, uint32_t q_sm) {
+  constexpr int SUB_BYTES = kBN * 128;
+  const int m = u.m0 + tile * kBM + row, token = m / p.group;
+  const bool live = m < u.rows;
+  const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + u.b * p.q_stride.batch +
+                                                    (long long)(u.kvh * p.group + m - token * p.group) * p.q_stride.head +
+                                                    (long long)token * p.q_stride.token);
+#pragma unroll 1
+  for (int first = 0; first < D / 8; first += 8) {
+    uint4 v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = live ? src[first + i] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t dst = q_sm + (first >> 3) * SUB_BYTES + row * 128 + ((i ^ (row & 7)) << 4);
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(__byte_perm(v[i].x, v[i].z, 0x5410)),
+                   "r"(__byte_perm(v[i].x, v[i].z, 0x7632)), "r"(__byte_perm(v[i].y, v[i].w, 0x5410)), "r"(__byte_perm(v[i].y, v[i].w, 0x7632)) : "memory");
+    }
+  }
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid_constant__ Kv4AttendParams p) {
   constexpr uint32_t SUB_BYTES = kBN * 128, TILE_BYTES = D / 64 * SUB_BYTES;      // tiles of 64 columns: 128 rows x 128 bytes
@@ -237,24 +260,15 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid
       }
     };
     uint32_t q_loads[2] = {0, 0};
-    // a tile of queries, a row a thread
-    auto queries = [&](int tile) {
-      const int row = tid & 127, m = unit->m0 + tile * kBM + row, token = m / p.group;
-      const bool live = m < unit->rows;
-      const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + unit->b * p.q_stride.batch +
-                                                        (long long)(unit->kvh * p.group + m - token * p.group) * p.q_stride.head +
-                                                        (long long)token * p.q_stride.token);
-      if (q_loads[tile] > 0 && !__all_sync(0xffffffffu, wait_bar(&bars->q_free[tile], (q_loads[tile] - 1) & 1, bars, polls))) return false;
-#pragma unroll 4
-      for (int chunk = 0; chunk < D / 8; ++chunk) {
-        const uint4 v = live ? src[chunk] : make_uint4(0, 0, 0, 0);
-        const uint32_t dst = q_sm + tile * TILE_BYTES + (chunk >> 3) * SUB_BYTES + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(__byte_perm(v.x, v.z, 0x5410)), "r"(__byte_perm(v.x, v.z, 0x7632)),
-                     "r"(__byte_perm(v.y, v.w, 0x5410)), "r"(__byte_perm(v.y, v.w, 0x7632)) : "memory");
+    // a tile of queries; those of the first unit come through the softmax warps, which have nothing else to do then
+    auto queries = [&](int tile, int n) {
+      if (n > 0) {
+        if (q_loads[tile] > 0 && !__all_sync(0xffffffffu, wait_bar(&bars->q_free[tile], (q_loads[tile] - 1) & 1, bars, polls))) return false;
+        load_queries<D>(p, *unit, tile, tid & 127, q_sm + tile * TILE_BYTES);
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bars->q_full[tile]));
       }
-      fence_proxy_async();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&bars->q_full[tile]));
       ++q_loads[tile];
       return true;
     };
@@ -287,7 +301,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid
         skip = unit->skip;
         last = unit->total - 1;
         load(0, 0);
-        ok = queries(0) && (unit->ntile == 1 || queries(1));
+        ok = queries(0, n) && (unit->ntile == 1 || queries(1, n));
 #pragma unroll 1
         for (int j = 0; j < nblk && ok; ++j) ok = turn(std::true_type(), j, 0, nblk) && turn(std::false_type(), j, 1, nblk);
         g += nblk;
@@ -318,6 +332,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid
       }
       const int nblk = u.nblk, j_begin = u.j_begin, seam = u.seam, skip = u.skip, total = u.total;
       const int all_lo = u.all_lo, all_hi = u.all_hi, all_sink = u.all_sink;
+      if (n == 0 && nblk > 0) {
+        load_queries<D>(p, u, t, row, q_sm + t * TILE_BYTES);
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bars->q_full[t]));
+      }
       float m_used = kNoLogit, l = 0.f;
 #pragma unroll 1
       for (int j = 0; j < nblk; ++j) {
