@@ -140,23 +140,32 @@ __device__ __forceinline__ void hide(uint32_t s_addr, int head, int seam, int hi
   tmem_wait_st();
 }
 
-// A row of a tile of queries into shared memory, elements in the order 0 4 1 5 2 6 3 7 of every eight.
-template <int D>
-__device__ __forceinline__ void load_queries(const Kv4AttendParams& p, const volatile Unit& u, int tile, int row, uint32_t q_sm) {
-  constexpr int SUB_BYTES = kBN * 128;
-  const int m = u.m0 + tile * kBM + row, token = m / p.group;
-  const bool live = m < u.rows;
-  const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.q) + u.b * p.q_stride.batch +
-                                                    (long long)(u.kvh * p.group + m - token * p.group) * p.q_stride.head +
-                                                    (long long)token * p.q_stride.token);
+// A tile of queries into shared memory by 128 threads, AHEAD loads of each in flight; elements in the order 0 4 1 5 2 6 3 7 of every
+// eight.  (A row a thread, 16 bytes of 32 rows an instruction, took 4 us.)
+template <int D, int AHEAD>
+__device__ __forceinline__ void load_queries(const Kv4AttendParams& p, const volatile Unit& u, int tile, int thread, uint32_t q_sm) {
+  constexpr int LPR = D / 8, RPT = 128 / LPR;            // threads of a row, rows of a turn
+  const int chunk = thread % LPR, rows = u.rows;
+  int m = u.m0 + tile * kBM + thread / LPR, token = m / p.group, g = m - token * p.group;
+  const int dt = RPT / p.group, dg = RPT - dt * p.group;
+  const __nv_bfloat16* const q = static_cast<const __nv_bfloat16*>(p.q) + u.b * p.q_stride.batch + (long long)(u.kvh * p.group) * p.q_stride.head + chunk * 8;
+  const uint32_t to = q_sm + (chunk >> 3) * (kBN * 128);
 #pragma unroll 1
-  for (int first = 0; first < D / 8; first += 8) {
-    uint4 v[8];
+  for (int first = thread / LPR; first < kBM; first += AHEAD * RPT) {
+    uint4 v[AHEAD];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = live ? src[first + i] : make_uint4(0, 0, 0, 0);
+    for (int i = 0; i < AHEAD; ++i) {
+      v[i] = make_uint4(0, 0, 0, 0);
+      if (m < rows) v[i] = *reinterpret_cast<const uint4*>(q + (long long)g * p.q_stride.head + (long long)token * p.q_stride.token);
+      m += RPT;
+      token += dt;
+      g += dg;
+      if (g >= p.group) { g -= p.group; ++token; }
+    }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t dst = q_sm + (first >> 3) * SUB_BYTES + row * 128 + ((i ^ (row & 7)) << 4);
+    for (int i = 0; i < AHEAD; ++i) {
+      const int row = first + i * RPT;
+      const uint32_t dst = to + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
       asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(__byte_perm(v[i].x, v[i].z, 0x5410)),
                    "r"(__byte_perm(v[i].x, v[i].z, 0x7632)), "r"(__byte_perm(v[i].y, v[i].w, 0x5410)), "r"(__byte_perm(v[i].y, v[i].w, 0x7632)) : "memory");
     }
@@ -264,7 +273,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid
     auto queries = [&](int tile, int n) {
       if (n > 0) {
         if (q_loads[tile] > 0 && !__all_sync(0xffffffffu, wait_bar(&bars->q_free[tile], (q_loads[tile] - 1) & 1, bars, polls))) return false;
-        load_queries<D>(p, *unit, tile, tid & 127, q_sm + tile * TILE_BYTES);
+        load_queries<D, 8>(p, *unit, tile, tid & 127, q_sm + tile * TILE_BYTES);
         fence_proxy_async();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&bars->q_full[tile]));
@@ -333,7 +342,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid
       const int nblk = u.nblk, j_begin = u.j_begin, seam = u.seam, skip = u.skip, total = u.total;
       const int all_lo = u.all_lo, all_hi = u.all_hi, all_sink = u.all_sink;
       if (n == 0 && nblk > 0) {
-        load_queries<D>(p, u, t, row, q_sm + t * TILE_BYTES);
+        load_queries<D, D / 8>(p, u, t, row, q_sm + t * TILE_BYTES);
         fence_proxy_async();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&bars->q_full[t]));
@@ -435,31 +444,36 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid
                                                (long long)token * p.out_stride.token);
       }
 #pragma unroll 1
-      for (int ch = 0; ch < D / 16; ++ch) {
-        uint32_t o[16];
+      for (int half = 0; half < D / 64; ++half) {
+        uint32_t o[64];
         if (nblk > 0) {
-          tmem_ld16(o_addr + ch * 16, o);
+          tmem_ld32(o_addr + half * 64, o);
+          tmem_ld32(o_addr + half * 64 + 32, o + 32);
           tmem_wait_ld();
         } else {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) o[i] = 0;
+          for (int i = 0; i < 64; ++i) o[i] = 0;
         }
-        // columns 0 4 1 5 2 6 3 7 of every eight
-        float y[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) y[i] = __uint_as_float(o[(i & 8) + 2 * (i & 3) + ((i >> 2) & 1)]);
         if (!live) continue;
-        if (part) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) reinterpret_cast<float4*>(part + ch * 16)[i] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
-        } else {
-          uint32_t w[8];
+        for (int ch = 0; ch < 4; ++ch) {
+          // columns 0 4 1 5 2 6 3 7 of every eight
+          float y[16];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const __nv_bfloat162 hh = __floats2bfloat162_rn(y[2 * i] * inv, y[2 * i + 1] * inv);
-            w[i] = *reinterpret_cast<const uint32_t*>(&hh);
+          for (int i = 0; i < 16; ++i) y[i] = __uint_as_float(o[16 * ch + (i & 8) + 2 * (i & 3) + ((i >> 2) & 1)]);
+          if (part) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              reinterpret_cast<float4*>(part + half * 64 + ch * 16)[i] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+          } else {
+            uint32_t w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const __nv_bfloat162 hh = __floats2bfloat162_rn(y[2 * i] * inv, y[2 * i + 1] * inv);
+              w[i] = *reinterpret_cast<const uint32_t*>(&hh);
+            }
+            st_global_32b(dst + half * 128 + ch * 32, w, p.out_sectors != 0);
           }
-          st_global_32b(dst + ch * 32, w, p.out_sectors != 0);
         }
       }
       tc_fence_before();                                           // (the next unit's products write there)
