@@ -165,34 +165,38 @@ lib = _load()
 
 
 def _load_call():
-    """call(address, handle, layer, scale, *buffers) -> status, invoke(address, *buffers) -> status and key(*tensors): the
-    compiled marshalling of the entry points that run step by step, or the same through ctypes if the module was not built for
-    this interpreter."""
+    """call(address, handle, layer, scale, *buffers) -> status and run(store, head, address, lead, stream, *tensors) -> status or
+    key: the compiled marshalling of the entry points that run step by step (csrc/pycall.c), or the same through ctypes if the module
+    was not built for this interpreter."""
     path = os.path.join(os.path.dirname(_LIB_PATH), "_hackcall" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
     if os.path.exists(path):
         spec = importlib.util.spec_from_file_location("_hackcall", path)
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
-        if hasattr(module, "invoke"):
-            return module.call, module.invoke, module.key
+        if hasattr(module, "run"):
+            return module.call, module.run
     functions = {_address(n): getattr(lib, n)
                  for n in ("hack_score", "hack_select", "hack_compact", "hack_attend", "hack_attend_variance",
-                           "hack_scale_step", "hack_scale_step_host") + _INVOKED}
-    return (lambda address, handle, layer, scale, *buffers: functions[address](handle, layer, scale, *map(_ptr, buffers)),
-            lambda address, *buffers: functions[address](*map(_ptr, buffers)),
-            lambda *tensors: tuple(None if x is None else (x.dtype, x.shape, x.stride(), x.get_device()) for x in tensors))
+                           "hack_scale_step", "hack_scale_step_host") + _RUN}
+
+    def run(store, head, address, lead, stream, *tensors):
+        key = (head,) + tuple(v for x in tensors for v in ((None,) * 4 if x is None else (x.dtype, x.shape, x.stride(), x.get_device())))
+        entry = store.get(key)
+        return key if entry is None else functions[address](_ptr(lead), entry[1], *map(_ptr, tensors), _ptr(stream))
+
+    return lambda address, handle, layer, scale, *buffers: functions[address](handle, layer, scale, *map(_ptr, buffers)), run
 
 
 def _address(name: str) -> int:
     return C.cast(getattr(lib, name), C.c_void_p).value
 
 
-_INVOKED = ("hack_rope", "hack_qk_norm_rope", "hack_kv4_append", "hack_kv4_read", "hack_kv4_attend")
-_call, _invoke, _key = _load_call()
+_RUN = ("hack_rope", "hack_qk_norm_rope", "hack_kv4_append", "hack_kv4_read", "hack_kv4_attend")
+_call, _run = _load_call()
 _SCORE, _SELECT, _COMPACT, _ATTEND, _ATTEND_VARIANCE, _SCALE_STEP, _SCALE_STEP_HOST = map(_address, (
     "hack_score", "hack_select", "hack_compact", "hack_attend", "hack_attend_variance", "hack_scale_step",
     "hack_scale_step_host"))
-_ROPE, _QK_NORM_ROPE, _KV4_APPEND, _KV4_READ, _KV4_ATTEND = map(_address, _INVOKED)
+_ROPE, _QK_NORM_ROPE, _KV4_APPEND, _KV4_READ, _KV4_ATTEND = map(_address, _RUN)
 
 
 def hack_last_error() -> str:
@@ -226,6 +230,15 @@ def hack_score_noalloc(q, k_cand, scores, n_rows: int, n_queries: int, n_cand: i
     """Scores on dense device tensors with no device allocation (fixed in-library scratch)."""
     _check(lib.hack_score_noalloc(_ptr(q), _ptr(k_cand), _ptr(scores), n_rows, n_queries, n_cand,
                                   score_stride, head_dim, dtype, n_obs, sm_scale, _ptr(stream)))
+
+
+def _ptr(x) -> Optional[int]:
+    """Raw address of a torch tensor / int / None."""
+    if x is None:
+        return None
+    if isinstance(x, int):
+        return x
+    return x.data_ptr()
 
 
 # ------------------------------------------------------------------ tensors [batch, heads, tokens, head_dim]
@@ -281,15 +294,11 @@ def _float_vector(x, n: int, device: int, what: str) -> None:
 _args_of = {}     # argument structs by shapes, strides and types: they hold nothing of a call's tensors
 
 
-def _cached(key, make):
-    """(struct, its address); the caller holds on to it for the call, as another thread may empty the store."""
-    args = _args_of.get(key)
-    if args is None:
-        if len(_args_of) >= 4096:
-            _args_of.clear()
-        made = make()
-        args = _args_of[key] = (made, C.addressof(made))
-    return args
+def _keep(key, args):
+    """The struct of a call that is seen for the first time."""
+    if len(_args_of) >= 4096:
+        _args_of.clear()
+    _args_of[key] = (args, C.addressof(args))
 
 
 def hack_rope_plan(head_dim: int, rotary_dim: Optional[int] = None, layout: int = HACK_ROPE_HALF, axes: int = 1,
@@ -304,21 +313,23 @@ def hack_rope_plan(head_dim: int, rotary_dim: Optional[int] = None, layout: int 
 def hack_rope(plan: HackRopePlan, x, y, positions, transpose: bool = False, stream=None) -> None:
     """y = x rotated to its tokens' positions.  x, y: [batch, heads, tokens, head_dim], any strides but the last; positions:
     int32 or float32 [batch,] tokens[, axes]."""
-    axes = plan.axes
-
-    def make():
-        _same("hack_rope", x, y)
-        b, h, n, d = x.shape
-        if tuple(y.shape) != (b, h, n, d) or d != plan.head_dim:
-            raise ValueError("x and y must have the same shape, with the plan's head_dim")
-        f32, stride = _positions(positions, b, n, axes, x.get_device())
-        return HackRopeArgs(x.get_device(), _dtype_of(x), b, h, n, int(transpose), f32, 0, stride, _strides_of(x, "x"),
-                            _strides_of(y, "y"))
-
-    args = _cached((axes, plan.head_dim, transpose, _key(x, y, positions)), make)
-    status = _invoke(_ROPE, C.addressof(plan), args[1], x, y, positions, stream)
+    head = ("rope", plan.axes, plan.head_dim, transpose)
+    status = _run(_args_of, head, _ROPE, C.addressof(plan), stream, x, y, positions)
+    if status.__class__ is tuple:
+        _keep(status, _rope_args(plan, x, y, positions, transpose))
+        status = _run(_args_of, head, _ROPE, C.addressof(plan), stream, x, y, positions)
     if status:
         _check(status)
+
+
+def _rope_args(plan, x, y, positions, transpose):
+    _same("hack_rope", x, y)
+    b, h, n, d = x.shape
+    if tuple(y.shape) != (b, h, n, d) or d != plan.head_dim:
+        raise ValueError("x and y must have the same shape, with the plan's head_dim")
+    f32, stride = _positions(positions, b, n, plan.axes, x.get_device())
+    return HackRopeArgs(x.get_device(), _dtype_of(x), b, h, n, int(transpose), f32, 0, stride, _strides_of(x, "x"),
+                        _strides_of(y, "y"))
 
 
 def _qkv_args(plan, q, k, v, q_out, k_out, v_out, positions, norm, eps, q_weight, k_weight, q_gain, k_gain):
@@ -346,22 +357,14 @@ def hack_qk_norm_rope(plan: Optional[HackRopePlan], q, k, v, q_out, k_out, v_out
                       eps: float = 1e-6, q_weight=None, k_weight=None, q_gain=None, k_gain=None, stream=None) -> None:
     """Queries and keys normalised per head, weighted and rotated, values copied: from views of a projection's output to the
     layout of the steps.  All tensors [batch, heads, tokens, head_dim]; plan and positions None: no rotation."""
-    args = _cached((None if plan is None else (plan.axes, plan.head_dim), norm, eps,
-                    _key(q, k, v, q_out, k_out, v_out, positions, q_weight, k_weight, q_gain, k_gain)),
-                   lambda: _qkv_args(plan, q, k, v, q_out, k_out, v_out, positions, norm, eps, q_weight, k_weight, q_gain, k_gain))
-    status = _invoke(_QK_NORM_ROPE, None if plan is None else C.addressof(plan), args[1], q, k, v, q_out, k_out, v_out, positions,
-                     q_weight, k_weight, q_gain, k_gain, stream)
+    head = ("qkv", None if plan is None else (plan.axes, plan.head_dim), norm, eps)
+    lead = None if plan is None else C.addressof(plan)
+    status = _run(_args_of, head, _QK_NORM_ROPE, lead, stream, q, k, v, q_out, k_out, v_out, positions, q_weight, k_weight, q_gain, k_gain)
+    if status.__class__ is tuple:
+        _keep(status, _qkv_args(plan, q, k, v, q_out, k_out, v_out, positions, norm, eps, q_weight, k_weight, q_gain, k_gain))
+        status = _run(_args_of, head, _QK_NORM_ROPE, lead, stream, q, k, v, q_out, k_out, v_out, positions, q_weight, k_weight, q_gain, k_gain)
     if status:
         _check(status)
-
-
-def _ptr(x) -> Optional[int]:
-    """Raw address of a torch tensor / int / None."""
-    if x is None:
-        return None
-    if isinstance(x, int):
-        return x
-    return x.data_ptr()
 
 
 class HackKv4:
@@ -387,9 +390,7 @@ class HackKv4:
         self._planes = HackKv4Planes(self.device, batch, n_kv_heads, dim, cap, 0, _ptr(row_off), _ptr(k_codes), _ptr(v_codes),
                                      _ptr(k_scales), _ptr(v_scales))
         self._address = C.addressof(self._planes)
-
-    def _key(self, *more):
-        return (self.device, self.batch, self.n_kv_heads, self.head_dim) + more
+        self._head = (self.device, batch, n_kv_heads, dim)
 
     def _lengths(self, x, n: int, what: str) -> None:
         if x is not None and (str(x.dtype) != "torch.int32" or x.numel() != n or not x.is_contiguous() or x.get_device() != self.device):
@@ -405,14 +406,18 @@ class HackKv4:
         return HackKv4Rows(_dtype_of(k), k.shape[2], _strides_of(k, "k"), _strides_of(v, "v"))
 
     def hack_kv4_append(self, k, v, lens, new_lens=None, stream=None) -> None:
-        args = _cached(self._key("rows", _key(k, v, lens, new_lens)), lambda: self._rows(k, v, lens, new_lens))
-        status = _invoke(_KV4_APPEND, self._address, args[1], k, v, lens, new_lens, stream)
+        status = _run(_args_of, self._head, _KV4_APPEND, self._address, stream, k, v, lens, new_lens)
+        if status.__class__ is tuple:
+            _keep(status, self._rows(k, v, lens, new_lens))
+            status = _run(_args_of, self._head, _KV4_APPEND, self._address, stream, k, v, lens, new_lens)
         if status:
             _check(status)
 
     def hack_kv4_read(self, k_out, v_out, first, stream=None) -> None:
-        args = _cached(self._key("rows", _key(k_out, v_out, first, None)), lambda: self._rows(k_out, v_out, first, None))
-        status = _invoke(_KV4_READ, self._address, args[1], k_out, v_out, first, stream)
+        status = _run(_args_of, self._head, _KV4_READ, self._address, stream, k_out, v_out, first)
+        if status.__class__ is tuple:
+            _keep(status, self._rows(k_out, v_out, first, None))
+            status = _run(_args_of, self._head, _KV4_READ, self._address, stream, k_out, v_out, first)
         if status:
             _check(status)
 
@@ -438,10 +443,14 @@ class HackKv4:
                         n_sink: int = 0, window: int = 0, sm_scale: float = 0.0, form: int = 0, stream=None) -> None:
         """q, out: [batch, heads, tokens, head_dim].  workspace: a uint8 tensor of hack_kv4_workspace bytes, or None where that
         is 0."""
-        room = 0 if workspace is None else workspace.numel() * workspace.element_size()
-        args = _cached(self._key(max_len, appended, causal, n_sink, window, sm_scale, room, form, _key(q, out, lens, new_lens)),
-                       lambda: self._attend(q, out, lens, max_len, new_lens, appended, causal, n_sink, window, sm_scale, room, form))
-        status = _invoke(_KV4_ATTEND, self._address, args[1], q, out, lens, new_lens, workspace if room else None, stream)
+        head = (self._head, max_len, appended, causal, n_sink, window, sm_scale, form)
+        status = _run(_args_of, head, _KV4_ATTEND, self._address, stream, q, out, lens, new_lens, workspace)
+        if status.__class__ is tuple:
+            room = 0 if workspace is None else workspace.numel() * workspace.element_size()
+            if room and (not workspace.is_contiguous() or workspace.get_device() != self.device):
+                raise ValueError("the workspace must be contiguous and on the cache's device")
+            _keep(status, self._attend(q, out, lens, max_len, new_lens, appended, causal, n_sink, window, sm_scale, room, form))
+            status = _run(_args_of, head, _KV4_ATTEND, self._address, stream, q, out, lens, new_lens, workspace)
         if status:
             _check(status)
 
@@ -541,10 +550,8 @@ class HackCache:
     def hack_scale_step_qkv(self, layer, scale, plan: Optional[HackRopePlan], q, k, v, out, positions, norm: int = HACK_NORM_RMS,
                             eps: float = 1e-6, q_weight=None, k_weight=None, q_gain=None, k_gain=None, stream=None) -> None:
         """hack_qk_norm_rope into buffers of the cache, then hack_scale_step."""
-        args = _cached((None if plan is None else (plan.axes, plan.head_dim), norm, eps, "step",
-                        _key(q, k, v, positions, q_weight, k_weight, q_gain, k_gain)),
-                       lambda: _qkv_args(plan, q, k, v, q, k, v, positions, norm, eps, q_weight, k_weight, q_gain, k_gain))
-        _check(lib.hack_scale_step_qkv(self._h, layer, scale, None if plan is None else C.addressof(plan), args[1], _ptr(q), _ptr(k),
+        args = _qkv_args(plan, q, k, v, q, k, v, positions, norm, eps, q_weight, k_weight, q_gain, k_gain)
+        _check(lib.hack_scale_step_qkv(self._h, layer, scale, None if plan is None else C.addressof(plan), C.addressof(args), _ptr(q), _ptr(k),
                                        _ptr(v), _ptr(positions), _ptr(q_weight), _ptr(k_weight), _ptr(q_gain), _ptr(k_gain), _ptr(out),
                                        _ptr(stream)))
 

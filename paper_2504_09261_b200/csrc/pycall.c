@@ -1,4 +1,4 @@
-/* Marshalling of the per-step calls from Python, in C: call(address, handle, layer, scale, buffer, ...)
+/* Marshalling of the per-step calls from Python, in C (run, of the operators around them: further down): call(address, handle, layer, scale, buffer, ...)
  * calls the entry point at `address` of the C ABI (hack.h) with three to five buffer arguments and
  * returns its status.  A buffer is None, an integer address or an object with a data_ptr() method.
  * The same call through ctypes takes 1.9 us of host time per step against 0.5; a small step keeps the GPU
@@ -48,47 +48,13 @@ static PyObject* call(PyObject* self, PyObject* const* args, Py_ssize_t n) {
   return PyLong_FromLong(status);
 }
 
-/* invoke(address, buffer, ...): an entry point whose arguments are all pointers. */
-static PyObject* invoke(PyObject* self, PyObject* const* args, Py_ssize_t n) {
-  (void)self;
-  if (n < 1 || n > 15) {
-    PyErr_SetString(PyExc_TypeError, "invoke(address, buffers...)");
-    return NULL;
-  }
-  void* fn = PyLong_AsVoidPtr(args[0]);
-  void* p[14] = {NULL};
-  if (PyErr_Occurred()) return NULL;
-  for (Py_ssize_t i = 1; i < n; ++i)
-    if (address_of(args[i], &p[i - 1])) return NULL;
-  int status = -1;
-#define P0_5 p[0], p[1], p[2], p[3], p[4], p[5]
-#define V6 void*, void*, void*, void*, void*, void*
-  Py_BEGIN_ALLOW_THREADS
-  switch (n - 1) {
-    case 6: status = ((int (*)(V6))fn)(P0_5); break;
-    case 7: status = ((int (*)(V6, void*))fn)(P0_5, p[6]); break;
-    case 8: status = ((int (*)(V6, void*, void*))fn)(P0_5, p[6], p[7]); break;
-    case 14: status = ((int (*)(V6, V6, void*, void*))fn)(P0_5, p[6], p[7], p[8], p[9], p[10], p[11], p[12], p[13]); break;
-  }
-  Py_END_ALLOW_THREADS
-#undef P0_5
-#undef V6
-  if (status < 0) {
-    PyErr_SetString(PyExc_TypeError, "invoke: 6, 7, 8 or 14 buffers");
-    return NULL;
-  }
-  return PyLong_FromLong(status);
-}
-
-/* key(tensor, ...): of each dtype, shape, strides and device, None for a None; what the arguments of a call that are not addresses
- * depend on.  In C because the same tuple costs a small call as much as its launch (eleven tensors: 9 us; here 4). */
-static PyObject* key(PyObject* self, PyObject* const* args, Py_ssize_t n) {
-  (void)self;
-  PyObject* out = PyTuple_New(4 * n);
-  if (!out) return NULL;
+/* What the arguments of a call that are not addresses depend on: of each tensor dtype, shape, strides and device, None for a None. */
+static PyObject* key_of(PyObject* head, PyObject* const* tensors, Py_ssize_t n) {
+  PyObject* key = PyTuple_New(1 + 4 * n);
+  if (!key) return NULL;
+  PyTuple_SET_ITEM(key, 0, Py_NewRef(head));
   for (Py_ssize_t i = 0; i < n; ++i) {
-    PyObject* x = args[i];
-    PyObject* got[4] = {NULL, NULL, NULL, NULL};
+    PyObject *x = tensors[i], *got[4] = {NULL, NULL, NULL, NULL};
     if (x == Py_None) {
       for (int k = 0; k < 4; ++k) got[k] = Py_NewRef(Py_None);
     } else {
@@ -97,17 +63,67 @@ static PyObject* key(PyObject* self, PyObject* const* args, Py_ssize_t n) {
       got[2] = got[1] ? PyObject_CallMethodNoArgs(x, stride_name) : NULL;
       got[3] = got[2] ? PyObject_CallMethodNoArgs(x, get_device_name) : NULL;
     }
-    for (int k = 0; k < 4; ++k) {
-      if (got[k]) { PyTuple_SET_ITEM(out, 4 * i + k, got[k]); continue; }
-      Py_DECREF(out);
+    if (!got[3]) {
+      for (int k = 0; k < 3; ++k) Py_XDECREF(got[k]);
+      Py_DECREF(key);
       return NULL;
     }
+    for (int k = 0; k < 4; ++k) PyTuple_SET_ITEM(key, 1 + 4 * i + k, got[k]);
   }
-  return out;
+  return key;
 }
 
-static PyMethodDef methods[] = {{"key", (PyCFunction)(void (*)(void))key, METH_FASTCALL, "key(tensors...) -> tuple"},
-                                {"invoke", (PyCFunction)(void (*)(void))invoke, METH_FASTCALL, "invoke(address, buffers...) -> status"},
+/* run(store, head, address, lead, stream, tensor, ...): the entry point at `address` with a lead pointer (a plan, a 4-bit cache), an
+ * argument struct, the tensors and the stream.  `store` maps keys (head, which is hashable, and what key_of says of the
+ * tensors) to (struct, its address).  Returns the entry point's status, or, where the store has no struct yet, the key. */
+static PyObject* run(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  (void)self;
+  const Py_ssize_t tensors = n - 5;
+  if (tensors < 3 || tensors > 11 || !PyDict_Check(args[0])) {
+    PyErr_SetString(PyExc_TypeError, "run(store, head, address, lead, stream, tensors...)");
+    return NULL;
+  }
+  void *p[14] = {NULL}, *fn = PyLong_AsVoidPtr(args[2]);
+  if (PyErr_Occurred() || address_of(args[3], &p[0])) return NULL;
+  PyObject* key = key_of(args[1], args + 5, tensors);
+  if (!key) return NULL;
+  PyObject* entry = PyDict_GetItemWithError(args[0], key);
+  if (!entry) {
+    if (!PyErr_Occurred()) return key;
+    Py_DECREF(key);
+    return NULL;
+  }
+  Py_INCREF(entry);                            /* (the struct lives on, whatever another thread does to the store) */
+  Py_DECREF(key);
+  p[1] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(entry, 1));
+  int bad = PyErr_Occurred() != NULL;
+  for (Py_ssize_t i = 0; i < tensors && !bad; ++i) bad = address_of(args[5 + i], &p[2 + i]);
+  if (!bad) bad = address_of(args[4], &p[2 + tensors]);
+  int status = -1;
+  if (!bad) {
+#define P0_5 p[0], p[1], p[2], p[3], p[4], p[5]
+#define V6 void*, void*, void*, void*, void*, void*
+    Py_BEGIN_ALLOW_THREADS
+    switch (tensors + 3) {
+      case 6: status = ((int (*)(V6))fn)(P0_5); break;
+      case 7: status = ((int (*)(V6, void*))fn)(P0_5, p[6]); break;
+      case 8: status = ((int (*)(V6, void*, void*))fn)(P0_5, p[6], p[7]); break;
+      case 14: status = ((int (*)(V6, V6, void*, void*))fn)(P0_5, p[6], p[7], p[8], p[9], p[10], p[11], p[12], p[13]); break;
+    }
+    Py_END_ALLOW_THREADS
+#undef P0_5
+#undef V6
+  }
+  Py_DECREF(entry);
+  if (bad) return NULL;
+  if (status < 0) {
+    PyErr_SetString(PyExc_TypeError, "run: 3, 4, 5 or 11 tensors");
+    return NULL;
+  }
+  return PyLong_FromLong(status);
+}
+
+static PyMethodDef methods[] = {{"run", (PyCFunction)(void (*)(void))run, METH_FASTCALL, "run(store, head, address, lead, stream, tensors...) -> status or key"},
                                 {"call", (PyCFunction)(void (*)(void))call, METH_FASTCALL, "call(address, handle, layer, scale, buffers...) -> status"},
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_hackcall", NULL, -1, methods, NULL, NULL, NULL, NULL};
