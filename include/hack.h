@@ -377,16 +377,18 @@ HACK_API hack_status_t hack_scale_step_qkv(hack_cache_t* cache, int32_t layer, i
  * 0, what is beyond 26 880 as that.
  * The planes are the caller's device buffers, 16-byte aligned: codes [rows, head_dim / 2] and scales
  * [rows, head_dim / 16] bytes of K and of V.  Head i = b * n_kv_heads + h owns rows
- * [first, first + cap), first = row_off[i] (device) or, row_off NULL, i * cap.  How many of them are
- * in use is the caller's to keep, on the device, so that a captured graph can be replayed with other
- * lengths: lens, int32 [batch * n_kv_heads].  The library only reads it; a length below 0 counts as
- * 0, one beyond cap as cap.
+ * [first, first + cap), first = row_off[i] (device) or, row_off NULL, i * cap.  A head whose rows are
+ * not all among the planes' `rows` counts as one without any; heads may share rows that are only read,
+ * those appended to must be a head's own.  How many of them are in use is the caller's to keep, on the
+ * device, so that a captured graph can be replayed with other lengths: lens, int32
+ * [batch * n_kv_heads].  The library only reads it; a length below 0 counts as 0, one beyond cap as cap.
  * new_lens (device, int32 [batch], may be NULL): of a padded batch, how many of the call's tokens each
  * batch element really has; the others are not read, and their outputs are left as they were.
  * ---------------------------------------------------------------------------------------------- */
 typedef struct {
   int32_t device, batch, n_kv_heads, head_dim;   /* head_dim 64 or 128 */
   int32_t cap, reserved;
+  int64_t rows;                                  /* of each plane */
   const int64_t* row_off;
   void *k_codes, *v_codes, *k_scales, *v_scales;
 } hack_kv4_t;
@@ -412,7 +414,8 @@ HACK_API hack_status_t hack_store_kv4(hack_cache_t* cache, int32_t layer, const 
 typedef struct {
   int32_t dtype;                 /* of q and out */
   int32_t n_heads, n_queries;    /* n_heads a multiple of n_kv_heads: query head h reads stored head h / (n_heads / n_kv_heads) */
-  int32_t max_len;               /* no head attends over more rows (launches are planned for it); rows behind it are not seen */
+  int32_t max_len;               /* no head attends over more rows (launches are planned for it): a longer one's length, which
+                                    the queries' positions go by as well, counts as this */
   int32_t appended;              /* 1: the n_queries (or new_lens[b]) rows behind lens count too: those just appended */
   int32_t causal;                /* 1: query i of n, at position length - n + i, sees no later rows */
   int32_t window, n_sink;        /* window > 0: of the rows up to its position a query sees the last `window` (itself

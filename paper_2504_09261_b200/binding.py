@@ -86,7 +86,7 @@ class HackQkvArgs(C.Structure):
 
 
 class HackKv4Planes(C.Structure):
-    _fields_ = [(n, C.c_int32) for n in ("device", "batch", "n_kv_heads", "head_dim", "cap", "reserved")] + [
+    _fields_ = [(n, C.c_int32) for n in ("device", "batch", "n_kv_heads", "head_dim", "cap", "reserved")] + [("rows", C.c_int64)] + [
         (n, C.c_void_p) for n in ("row_off", "k_codes", "v_codes", "k_scales", "v_scales")]
 
 
@@ -387,7 +387,7 @@ class HackKv4:
             raise ValueError("row_off must be batch * n_kv_heads contiguous int64 values on the planes' device")
         self.batch, self.n_kv_heads, self.cap, self.head_dim, self.device = batch, n_kv_heads, cap, dim, k_codes.get_device()
         self._held = (k_codes, k_scales, v_codes, v_scales, row_off)
-        self._planes = HackKv4Planes(self.device, batch, n_kv_heads, dim, cap, 0, _ptr(row_off), _ptr(k_codes), _ptr(v_codes),
+        self._planes = HackKv4Planes(self.device, batch, n_kv_heads, dim, cap, 0, rows, _ptr(row_off), _ptr(k_codes), _ptr(v_codes),
                                      _ptr(k_scales), _ptr(v_scales))
         self._address = C.addressof(self._planes)
         self._head = (self.device, batch, n_kv_heads, dim)

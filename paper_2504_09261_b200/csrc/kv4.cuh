@@ -17,6 +17,7 @@ constexpr uint32_t kScaleBias = (127 - 20) << 7;
 struct Planes {
   unsigned char *k_codes, *v_codes, *k_scales, *v_scales;
   const int64_t* row_off;
+  long long rows;
   int cap;
 };
 
@@ -24,6 +25,8 @@ struct Planes {
 __device__ __forceinline__ long long first_row(const Planes& p, int head) {
   return p.row_off ? (long long)p.row_off[head] : (long long)head * p.cap;
 }
+// Whether a head's rows are in the planes
+__device__ __forceinline__ bool inside(const Planes& p, long long first) { return first >= 0 && first <= p.rows - p.cap; }
 __device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float(((byte << 4) + kScaleBias) << 16); }
 __device__ __forceinline__ uint32_t bf162_mul(uint32_t a, uint32_t b) {
   uint32_t d;

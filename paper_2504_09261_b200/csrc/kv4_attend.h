@@ -36,6 +36,7 @@ struct Kv4Range { int sink_end, lo, hi, all_lo, all_hi, all_sink; };
 __device__ __forceinline__ int kv4_length(const Kv4AttendParams& p, int head, int nq) {
   // (64 bits: a length next to the end of 32 must not wrap)
   const long long len = (long long)max(p.lens[head], 0) + (p.appended ? nq : 0);
+  if (p.planes.row_off && !kv4::inside(p.planes, (long long)p.planes.row_off[head])) return 0;
   return (int)min(len, (long long)min(p.max_len, p.planes.cap));
 }
 // Of the query rows first .. last of a head (row = token * group + head of the group)

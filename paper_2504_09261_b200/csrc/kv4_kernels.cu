@@ -187,8 +187,9 @@ __global__ void __launch_bounds__(kThreads) kv4_append_kernel(const __grid_const
   rk.load(k, p.whole);
   rv.load(v, p.whole);
   const long long slot = (long long)max(p.lens[head], 0) + token;
-  if (slot >= p.planes.cap) return;
-  const long long at = (first_row(p.planes, head) + slot) * BLOCKS + block;
+  const long long first = first_row(p.planes, head);
+  if (slot >= p.planes.cap || !inside(p.planes, first)) return;
+  const long long at = (first + slot) * BLOCKS + block;
   uint32_t byte;
   uint2 code = quantise(rk, byte);
   reinterpret_cast<uint2*>(p.planes.k_codes)[at] = code;
@@ -237,8 +238,9 @@ __global__ void __launch_bounds__(kThreads) kv4_read_kernel(const __grid_constan
   const long long slot = (long long)p.lens[head] + token;
   uint2 kc = make_uint2(0x88888888u, 0x88888888u), vc = kc;      // code 8 stands for 0
   uint32_t kb = 0, vb = 0;
-  if (slot >= 0 && slot < p.planes.cap) {
-    const long long at = (first_row(p.planes, head) + slot) * BLOCKS + block;
+  const long long first = first_row(p.planes, head);
+  if (slot >= 0 && slot < p.planes.cap && inside(p.planes, first)) {
+    const long long at = (first + slot) * BLOCKS + block;
     kc = reinterpret_cast<const uint2*>(p.planes.k_codes)[at];
     vc = reinterpret_cast<const uint2*>(p.planes.v_codes)[at];
     kb = p.planes.k_scales[at];
@@ -310,6 +312,7 @@ hack_status_t kv4_check(const hack_kv4_t* kv) {
   if (kv->head_dim != 64 && kv->head_dim != 128) { set_error("head_dim must be 64 or 128"); return HACK_ERR_UNSUPPORTED; }
   if (kv->device < 0 || kv->batch < 1 || kv->n_kv_heads < 1 || kv->cap < 1 || (long long)kv->batch * kv->n_kv_heads > 0x7fffffffll)
     return invalid("batch, n_kv_heads and cap must be positive, device not negative");
+  if (kv->rows < kv->cap || (!kv->row_off && kv->rows < (long long)kv->batch * kv->n_kv_heads * kv->cap)) return invalid("the planes have too few rows");
   const void* planes[4] = {kv->k_codes, kv->v_codes, kv->k_scales, kv->v_scales};
   for (const void* q : planes)
     if (!q || (reinterpret_cast<uintptr_t>(q) & 15)) return invalid("a plane is NULL or not 16-byte aligned");
@@ -318,7 +321,7 @@ hack_status_t kv4_check(const hack_kv4_t* kv) {
 
 kv4::Planes kv4_planes(const hack_kv4_t* kv) {
   return {static_cast<unsigned char*>(kv->k_codes), static_cast<unsigned char*>(kv->v_codes),
-          static_cast<unsigned char*>(kv->k_scales), static_cast<unsigned char*>(kv->v_scales), kv->row_off, kv->cap};
+          static_cast<unsigned char*>(kv->k_scales), static_cast<unsigned char*>(kv->v_scales), kv->row_off, (long long)kv->rows, kv->cap};
 }
 
 hack_status_t launch_store_kv4(const StepArgs& a, int dtype, const hack_kv4_t* kv, const int32_t* lens, cudaStream_t st) {

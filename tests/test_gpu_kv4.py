@@ -133,6 +133,29 @@ def test_append_strided_padded_and_full(hb):
     assert (out[0][1] == 0).all() and (out[1][2, 0] == 0).all() and torch.isfinite(out[0]).all()
 
 
+def test_heads_outside_the_planes_have_no_rows(hb):
+    g = _gen(33)
+    heads, dim, cap, rows = 4, 64, 20, 60
+    planes = Planes(rows, dim)
+    planes.randomise(g)
+    before = [p.clone() for p in planes.all()]
+    row_off = torch.tensor([40, 41, -1, 2 ** 62], dtype=torch.int64, device="cuda")
+    kv4 = planes.handle(hb, 1, heads, cap, row_off)
+    k = torch.randn(1, heads, 3, dim, generator=g, device="cuda")
+    kv4.hack_kv4_append(k, k, _ints(0, 0, 0, 0))
+    back = [torch.full_like(k, 9.0) for _ in range(2)]
+    kv4.hack_kv4_read(*back, _ints(0, 0, 0, 0))
+    assert torch.equal(back[0][0, 0].double(), ref.quantise(k[0, 0])[2]) and (back[0][0, 1:] == 0).all() and (back[1][0, 1:] == 0).all()
+    for p, b in zip(planes.all(), before):
+        assert torch.equal(p[:40], b[:40]) and torch.equal(p[43:], b[43:])
+    for dtype, form in ((torch.float32, 1), (torch.bfloat16, 1), (torch.bfloat16, 2)):
+        q = torch.randn(1, heads, 5, dim, generator=g, device="cuda").to(dtype)
+        out = torch.full_like(q, 9.0)
+        kv4.hack_kv4_attend(q, out, _ints(3, 20, 20, 20), cap, workspace=torch.empty(1 << 22, dtype=torch.uint8, device="cuda"), form=form)
+        want = ref.attend(q[0, :1], ref.quantise(k[0, 0])[2], ref.quantise(k[0, 0])[2], 3, 5, dim ** -0.5)
+        assert ((out[0, :1].double() - want[0]).abs() <= ref.bound(*want, dtype, dim, 3)).all() and (out[0, 1:] == 0).all()
+
+
 # ------------------------------------------------------------------ attention
 def _check(hb, g, dtype, dim, batch, kv_heads, group, tokens, cap, lens, max_len=None, causal=False, window=0, n_sink=0, new_lens=None,
            appended=False, sm_scale=0.0, row_off=None, rows=None, q_layout="token", q_size=1.0, planes=None, form=0):

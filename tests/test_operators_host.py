@@ -85,14 +85,14 @@ def test_qk_norm_rope_refuses(hb, change, status):
 
 def _kv4(**change):
     from paper_2504_09261_b200 import binding as bd
-    f = dict(device=0, batch=2, n_kv_heads=3, head_dim=128, cap=50, reserved=0, row_off=None, k_codes=4096, v_codes=8192, k_scales=12288,
+    f = dict(device=0, batch=2, n_kv_heads=3, head_dim=128, cap=50, reserved=0, rows=300, row_off=None, k_codes=4096, v_codes=8192, k_scales=12288,
              v_scales=16384)
     f.update(change)
     return bd.HackKv4Planes(*f.values())
 
 
 @pytest.mark.parametrize("change,status", [(dict(head_dim=32), 2), (dict(batch=0), 1), (dict(n_kv_heads=-1), 1), (dict(cap=0), 1), (dict(device=-2), 1),
-                                           (dict(k_codes=None), 1), (dict(v_scales=16392), 1), (dict(batch=1 << 20, n_kv_heads=1 << 12), 1)])
+                                           (dict(k_codes=None), 1), (dict(rows=299), 1), (dict(rows=49, row_off=4096), 1), (dict(v_scales=16392), 1), (dict(batch=1 << 20, n_kv_heads=1 << 12), 1)])
 def test_kv4_planes_refused(hb, change, status):
     from paper_2504_09261_b200 import binding as bd
     kv, rows = _kv4(**change), bd.HackKv4Rows(1, 4, bd.HackStrides(1536, 512, 128), bd.HackStrides(1536, 512, 128))
