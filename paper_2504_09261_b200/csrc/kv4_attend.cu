@@ -433,12 +433,10 @@ __global__ void __launch_bounds__(kCombineThreads) kv4_combine_kernel(const __gr
   __shared__ float weight[kMaxSplits];
   __shared__ float4 sums[GROUPS][LANES];
   pdl_wait();
-  const int unit = blockIdx.x / p.tile_rows, row = blockIdx.x - unit * p.tile_rows;
-  const int head = unit / p.tiles, tile = unit - head * p.tiles;
+  const int rows = p.n_queries * p.group, head = blockIdx.x / rows, m = blockIdx.x - head * rows;
+  const int tile = m / p.tile_rows, row = m - tile * p.tile_rows, unit = head * p.tiles + tile;
   const int b = head / p.kv_heads, kvh = head - b * p.kv_heads;
-  const int nq = p.new_lens ? min(max(p.new_lens[b], 0), p.n_queries) : p.n_queries;
-  const int m = tile * p.tile_rows + row;
-  if (m >= nq * p.group) return;
+  if (p.new_lens && m >= p.new_lens[b] * (long long)p.group) return;
   const long long step = (long long)p.tile_rows * (D + 2);
   const float* part = p.partial + (long long)unit * p.splits * step;
   const int lane = threadIdx.x & 31, group = threadIdx.x / LANES, d = (threadIdx.x % LANES) * 4;
@@ -503,7 +501,7 @@ int launch_attend(const Kv4AttendParams& p, cudaStream_t st) {
   const int r = p.tile_rows == 8 ? launch_few<D, F32, 1>(p, st) : p.tile_rows == 16 ? launch_few<D, F32, 2>(p, st) : launch_kv4_attend_tc(p, D, st);
   if (r < 0) return -1;
   if (p.splits > 1) {
-    launch_k(kv4_combine_kernel<D, F32>, dim3((unsigned)p.units * p.tile_rows), dim3(kCombineThreads), 0, st, p);
+    launch_k(kv4_combine_kernel<D, F32>, dim3((unsigned)(p.units / p.tiles) * p.n_queries * p.group), dim3(kCombineThreads), 0, st, p);
   }
   return launched(1);
 }
@@ -576,7 +574,8 @@ hack_status_t plan(const hack_kv4_t* kv, const hack_kv4_attend_t* a, Kv4AttendPa
       if (n == 1 || cost < best) { best = cost; p.splits = n; }
     }
   }
-  p.wait_polls = a->wait_polls > 0 ? (uint32_t)a->wait_polls : kWaitPolls;
+  // (a role may wait for a whole unit of work: some sixty polls a block)
+  p.wait_polls = a->wait_polls > 0 ? (uint32_t)a->wait_polls : kWaitPolls + (uint32_t)std::min<long long>(walked, 1 << 30);
   workspace = p.splits > 1 ? (size_t)p.units * p.splits * p.tile_rows * (kv->head_dim + 2) * 4 : 0;
   return HACK_OK;
 }
