@@ -11,7 +11,8 @@
 // and the queries its eight columns (K Q^T, then V^T P^T): one query, or the few that share a stored head, leave as little of it
 // empty as can be, and hold half the registers of the other way round.  Softmax with a running maximum that is
 // raised only when a logit exceeds it by 2^16; a CTA's warps are merged in shared memory, CTAs that share the rows of a head
-// (`splits`) through partial results in the workspace, which kv4_combine_kernel adds up.
+// (`splits`) as a cluster, through each other's shared memory, or through partial results in the workspace, which kv4_combine_kernel
+// adds up.
 // bf16: a probability is rounded once for the product with the values, which costs as much accuracy again as the rounding of the
 // result; as the sum of two bf16 numbers it costs a tenth of the time instead (32 heads of up to 65 536 rows 63 and 70 us).  fp32:
 // queries and probabilities as sums of three bf16 numbers, which is all of their 24 bits.
@@ -33,7 +34,7 @@ using ptx::ex2;
 using ptx::smem_u32;
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
-constexpr int kCombineThreads = 256, kMaxSplits = 64;
+constexpr int kCombineThreads = 256, kMaxSplits = 64, kMaxCluster = 8;
 constexpr int kChunk = 32;                   // stored rows of a turn of a warp
 constexpr int kStages = 3;
 constexpr float kRaise = 16.f;               // log2 by which a logit may exceed the reference maximum
@@ -64,6 +65,26 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   return y;
 }
 
+// Shared memory of a cluster's CTAs
+__device__ __forceinline__ uint32_t at_rank(uint32_t addr, int rank) {
+  uint32_t x;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(x) : "r"(addr), "r"(rank));
+  return x;
+}
+__device__ __forceinline__ float4 load_shared4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ float2 load_shared2(uint32_t addr) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
 template <int D> struct Ring {
   static constexpr int kCodes = kChunk * D / 2, kScales = kChunk * D / 16;   // bytes of a chunk, of K or V
   static constexpr int kStage = 2 * (kCodes + kScales);
@@ -71,7 +92,7 @@ template <int D> struct Ring {
 };
 // The ring, later the warps' outputs; fp32: the query's fragments behind it.
 template <int D, bool F32, int NQ> constexpr size_t smem_bytes() {
-  constexpr size_t ring = (size_t)kWarps * Ring<D>::kWarp, merge = (size_t)kWarps * 8 * NQ * D * 4;
+  constexpr size_t ring = (size_t)kWarps * Ring<D>::kWarp, merge = (size_t)(kWarps + 1) * 8 * NQ * D * 4;
   return (ring > merge ? ring : merge) + (F32 ? 3 * NQ * (D / 16) * 32 * 8 : 0);
 }
 
@@ -87,6 +108,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(F32, NQ)) kv4_attend_ker
   constexpr int CODES = Ring<D>::kCodes, SCALES = Ring<D>::kScales;
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ float merge_m[kWarps][ROWS], merge_l[kWarps][ROWS];
+  __shared__ float2 cta_stats[ROWS];         // clusters: the CTA's reference maximum and sum of every row
   pdl_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, t = lane & 3;
   const int split = blockIdx.x, unit = blockIdx.y + blockIdx.z * gridDim.y;
@@ -399,6 +421,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(F32, NQ)) kv4_attend_ker
             make_float4(o[g][i][e] * f, o[g][i][2 + e] * f, o[g][i + 1][e] * f, o[g][i + 1][2 + e] * f);
     }
   __syncthreads();
+  float* const cta_out = reinterpret_cast<float*>(smem) + kWarps * ROWS * D;   // clusters: the CTA's outputs, behind the warps'
 #pragma unroll 1
   for (int x = threadIdx.x; x < ROWS * D / 4; x += kThreads) {
     const int row = x / (D / 4), d = (x - row * (D / 4)) * 4;
@@ -412,17 +435,52 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(F32, NQ)) kv4_attend_ker
       total += merge_l[w][row];
       mx = fmaxf(mx, merge_m[w][row]);
     }
-    if (p.splits > 1) {
+    if (p.splits == 1) {
+      kv4_store<F32>(p, b, kvh, m0 + row, d, sum, total);
+    } else if (p.clustered) {
+      *reinterpret_cast<float4*>(cta_out + row * D + d) = sum;
+      if (d == 0) cta_stats[row] = make_float2(mx, total);
+    } else {
       float* part = p.partial + ((long long)unit * p.splits + split) * (ROWS * (D + 2));
       *reinterpret_cast<float4*>(part + row * D + d) = sum;
       if (d == 0) {
         part[ROWS * D + 2 * row] = mx;
         part[ROWS * D + 2 * row + 1] = total;
       }
-    } else {
-      kv4_store<F32>(p, b, kvh, m0 + row, d, sum, total);
     }
   }
+  if (!p.clustered) return;
+  // ---- the cluster's shares: every CTA adds up a part of the outputs from all of them
+  cluster_barrier();
+  const int per = (ROWS * D / 4 + p.splits - 1) / p.splits;
+#pragma unroll 1
+  for (int i = threadIdx.x; i < per; i += kThreads) {
+    const int x = split * per + i, row = x / (D / 4), d = (x - row * (D / 4)) * 4;
+    if (row >= ROWS || m0 + row >= rows) break;
+    const uint32_t out_at = smem_u32(cta_out + row * D + d), stats_at = smem_u32(&cta_stats[row]);
+    float2 stats[kMaxCluster];
+    float4 v[kMaxCluster];
+    float mx = kNoLogit, total = 0.f;
+#pragma unroll
+    for (int s = 0; s < kMaxCluster; ++s) {
+      if (s >= p.splits) break;
+      stats[s] = load_shared2(at_rank(stats_at, s));
+      v[s] = load_shared4(at_rank(out_at, s));
+    }
+#pragma unroll
+    for (int s = 0; s < kMaxCluster; ++s)
+      if (s < p.splits) mx = fmaxf(mx, stats[s].x);
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int s = 0; s < kMaxCluster; ++s) {
+      if (s >= p.splits) break;
+      const float f = ex2((stats[s].x - mx) * c);
+      total += f * stats[s].y;
+      sum.x = fmaf(f, v[s].x, sum.x); sum.y = fmaf(f, v[s].y, sum.y); sum.z = fmaf(f, v[s].z, sum.z); sum.w = fmaf(f, v[s].w, sum.w);
+    }
+    kv4_store<F32>(p, b, kvh, m0 + row, d, sum, total);
+  }
+  cluster_barrier();                         // (the others may still read this CTA's)
 }
 
 // Partial results of the splits (at most 64) added up: a CTA for a query row, its groups of D / 4 threads share the splits.  (One
@@ -492,7 +550,25 @@ int launch_few(const Kv4AttendParams& p, cudaStream_t st) {
   constexpr size_t smem = smem_bytes<D, F32, NQ>();
   if (!allow_dynamic_smem(kv4_attend_kernel<D, F32, NQ>, smem)) return -1;
   const int y = std::min(p.units, 32768);
-  launch_k(kv4_attend_kernel<D, F32, NQ>, dim3(p.splits, y, (p.units + y - 1) / y), dim3(kThreads), smem, st, p);
+  const dim3 grid(p.splits, y, (p.units + y - 1) / y);
+  if (!p.clustered) {
+    launch_k(kv4_attend_kernel<D, F32, NQ>, grid, dim3(kThreads), smem, st, p);
+    return 1;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = p.splits;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  cudaLaunchKernelEx(&cfg, kv4_attend_kernel<D, F32, NQ>, p);
   return 1;
 }
 
@@ -500,7 +576,7 @@ template <int D, bool F32>
 int launch_attend(const Kv4AttendParams& p, cudaStream_t st) {
   const int r = p.tile_rows == 8 ? launch_few<D, F32, 1>(p, st) : p.tile_rows == 16 ? launch_few<D, F32, 2>(p, st) : launch_kv4_attend_tc(p, D, st);
   if (r < 0) return -1;
-  if (p.splits > 1) {
+  if (p.splits > 1 && !p.clustered) {
     launch_k(kv4_combine_kernel<D, F32>, dim3((unsigned)(p.units / p.tiles) * p.n_queries * p.group), dim3(kCombineThreads), 0, st, p);
   }
   return launched(1);
@@ -563,20 +639,33 @@ hack_status_t plan(const hack_kv4_t* kv, const hack_kv4_attend_t* a, Kv4AttendPa
     const long long ctas = (long long)heads * ((p.tiles + p.tiles_per_cta - 1) / p.tiles_per_cta);
     p.splits = (int)std::max<long long>(1, std::min<long long>({(walked + 127) / 128 / 4, sms / ctas, kMaxSplits}));
   } else {
-    // CTAs that share a unit's rows: as few turns one behind the other as can be, counting what a CTA, a second launch and a
-    // share in it cost in turns
+    // CTAs that share a unit's rows, in a cluster or with a second launch: the least of estimated us, fitted to both.  A turn
+    // (a chunk a warp) takes the longer the more CTAs an SM has, what follows the turns 2 or 2.7 us and more.  (us in a cluster and
+    // with a second launch: 128 heads of 2 240 rows x 64, two CTAs 9.8 and 10.9, four 9.9 and 10.7; 32 heads of 4 096 rows x 128,
+    // eight CTAs 9.5 and 10.0.  Clusters of other sizes may, and more than fit at once do find their places late: 128 heads, three
+    // and five CTAs 11.3 and 13.3; 32 heads, sixteen 13.4 where a second launch takes 10.3.)
     const long long turns = std::max<long long>(1, (walked + kChunk * kWarps - 1) / (kChunk * kWarps));
-    const long long places = (long long)sms * ctas_per_sm(a->dtype == HACK_F32, p.tile_rows / 8);
+    const int per_sm = ctas_per_sm(a->dtype == HACK_F32, p.tile_rows / 8);
+    const double turn_us = (wide ? 1.0 : 0.6) * (a->dtype == HACK_F32 ? 0.8 * (p.tile_rows / 8) + 0.7 : p.tile_rows == 16 ? 1.4 : 1.0);
     double best = 0;
     p.splits = 1;
     for (int n = 1; n <= kMaxSplits && n <= turns; ++n) {
-      const double cost = (double)((units * n + places - 1) / places) * ((double)((turns + n - 1) / n) + 3.0) + (n > 1 ? 3.0 + 0.1 * n : 0.0);
-      if (n == 1 || cost < best) { best = cost; p.splits = n; }
+      const long long ctas = units * n, places = (long long)sms * per_sm;
+      const int on_sm = (int)std::min<long long>(per_sm, (ctas + sms - 1) / sms);
+      const double waves = n == 1 ? std::max(1.0, (double)ctas / places) : (double)((ctas + places - 1) / places);
+      const double work = waves * ((double)((turns + n - 1) / n) * turn_us * (0.55 + 0.38 * on_sm) + 2.2);
+      const bool cluster = n > 1 && n <= kMaxCluster && ctas <= places;
+      const double cost = work + (n == 1 ? 0.0 : cluster ? 2.0 + ((n & (n - 1)) ? 1.0 : 0.0) : 2.7 + 0.03 * n);
+      if (n == 1 || cost < best) {
+        best = cost;
+        p.splits = n;
+        p.clustered = cluster;
+      }
     }
   }
   // (a role may wait for a whole unit of work: some sixty polls a block)
   p.wait_polls = a->wait_polls > 0 ? (uint32_t)a->wait_polls : kWaitPolls + (uint32_t)std::min<long long>(walked, 1 << 30);
-  workspace = p.splits > 1 ? (size_t)p.units * p.splits * p.tile_rows * (kv->head_dim + 2) * 4 : 0;
+  workspace = p.splits > 1 && !p.clustered ? (size_t)p.units * p.splits * p.tile_rows * (kv->head_dim + 2) * 4 : 0;
   return HACK_OK;
 }
 

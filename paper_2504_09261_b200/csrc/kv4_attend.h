@@ -12,6 +12,7 @@ struct Kv4AttendParams {
   int causal, window, n_sink, appended;
   int tile_rows;                    // query rows of a tile: 8 or 16, or 128 on the tensor cores
   int tiles, units, splits;         // tiles of query rows of a stored head, all of them, CTAs that share the rows of one
+  int clustered;                    // few rows: they are a cluster
   int tiles_per_cta;                // tensor cores: 1 or 2
   int steal;                        // tensor cores: more units than CTAs run at once, a CTA goes on with another one
   int out_sectors;                  // rows of the output start on 32-byte boundaries

@@ -322,7 +322,7 @@ def test_graph_replayed_with_other_lengths(hb):
 
 def test_two_streams_with_workspaces_of_their_own(hb):
     g = _gen(13)
-    dim, cap = 64, 9000
+    dim, cap = 64, 60000
     planes = Planes(2 * cap, dim)
     planes.randomise(g)
     kv4 = planes.handle(hb, 1, 2, cap)
