@@ -441,8 +441,9 @@ class HackKv4:
 
     def hack_kv4_attend(self, q, out, lens, max_len: int, workspace=None, new_lens=None, appended: bool = False, causal: bool = False,
                         n_sink: int = 0, window: int = 0, sm_scale: float = 0.0, form: int = 0, stream=None) -> None:
-        """q, out: [batch, heads, tokens, head_dim].  workspace: a uint8 tensor of hack_kv4_workspace bytes, or None where that
-        is 0."""
+        """q, out: [batch, heads, tokens, head_dim].  max_len: any bound of the lengths (one that is rounded up, rather than another
+        in every step, spares the host a new argument struct).  workspace: a uint8 tensor of hack_kv4_workspace bytes, or None
+        where that is 0."""
         head = (self._head, max_len, appended, causal, n_sink, window, sm_scale, form)
         status = _run(_args_of, head, _KV4_ATTEND, self._address, stream, q, out, lens, new_lens, workspace)
         if status.__class__ is tuple:

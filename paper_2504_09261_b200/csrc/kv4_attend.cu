@@ -2,7 +2,7 @@
 //
 // A stored element is c * s with c of four bits and s of four significant bits, which bf16 holds exactly: the matrix
 // instructions see what is stored, not a rounding of it.  The query rows of the heads that share a stored head are the rows
-// of one product: m = token * group + head, in tiles of 16.
+// of one product: m = token * group + head, in tiles of 8, 16 or 128.
 //
 // kv4_attend_kernel: few rows, or fp32.  A warp takes chunks of 32 stored rows through a ring of its own in shared memory
 // (cp.async, so that neither their place nor the end of a head has to be aligned); its lanes read the codes there in the
@@ -287,7 +287,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(F32, NQ)) kv4_attend_ker
       }
     }
     // ---- softmax
-    if (first + kChunk > end || !kv4_all_see(p, range, first)) {
+    if (first + kChunk > end || !kv4_all_see(range, first)) {
 #pragma unroll
       for (int g = 0; g < NQ; ++g)
 #pragma unroll
@@ -615,9 +615,11 @@ hack_status_t plan(const hack_kv4_t* kv, const hack_kv4_attend_t* a, Kv4AttendPa
   p.n_sink = a->window > 0 ? std::min(a->n_sink, 1 << 30) : 0;
   p.appended = a->appended != 0;
   const int heads = kv->batch * kv->n_kv_heads, rows = a->n_queries * p.group;
-  // rows that a tile of queries walks at most
+  // rows that a unit's queries, 256 rows of them at most, walk at most (us with those of all queries counted, and of a unit's:
+  // 8 query heads of 1 024 tokens on 2 stored ones x 128, a window of 256, 31.6 and 19.4; 2 heads, a window of 1 024, 19.4 and 14.7)
   long long walked = p.max_len;
-  if (p.window > 0) walked = std::min<long long>(walked, (long long)p.window + p.n_sink + p.n_queries);
+  if (p.window > 0)
+    walked = std::min<long long>(walked, (long long)p.window + p.n_sink + (p.causal ? std::min(p.n_queries, 256 / p.group + 2) : p.n_queries));
   // Which kernel: estimated us of a launch in one wave or more, fitted to both forms (us, few-rows form and tensor cores: 16 heads of
   // 10 521 rows x 128, 32 queries 22.1 and 25.8, 48 26.8 and 26.6, 64 35.3 and 27.3; 64 heads of 2 240 rows, 48 queries 31.9 and 34.4,
   // 64 38.9 and 35.9; 4 heads of 700 rows x 64, 64 queries 6.3 and 12.9; 128 heads of 680 rows 14.9 and 14.1).

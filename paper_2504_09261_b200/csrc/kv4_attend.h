@@ -55,7 +55,7 @@ __device__ __forceinline__ Kv4Range kv4_range(const Kv4AttendParams& p, int len,
 // Runs of `size` rows that cover it
 __device__ __forceinline__ int kv4_chunks(const Kv4Range& r, int size) { return (r.sink_end + size - 1) / size + (r.hi - r.lo + size - 1) / size; }
 // Whether every query row of the tile sees the 32 rows from `first` on
-__device__ __forceinline__ bool kv4_all_see(const Kv4AttendParams&, const Kv4Range& r, int first) {
+__device__ __forceinline__ bool kv4_all_see(const Kv4Range& r, int first) {
   return first + 32 <= r.all_hi && (first >= r.all_lo || first + 32 <= r.all_sink);
 }
 // Whether a query at position `at` sees `row` (below the length)
