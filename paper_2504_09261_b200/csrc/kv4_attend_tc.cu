@@ -188,7 +188,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid
   if (tid == 0) {
     for (int t = 0; t < 2; ++t) {
       mbar_init(smem_u32(&bars->u_full[t]), 1);
-      mbar_init(smem_u32(&bars->u_empty[t]), 14);      mbar_init(smem_u32(&bars->q_full[t]), 4);
+      mbar_init(smem_u32(&bars->u_empty[t]), 14);
+      mbar_init(smem_u32(&bars->q_full[t]), 4);
       mbar_init(smem_u32(&bars->q_free[t]), 1);
       mbar_init(smem_u32(&bars->s_full[t]), 1);
       mbar_init(smem_u32(&bars->p_full[t]), 4);
