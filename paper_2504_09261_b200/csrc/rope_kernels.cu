@@ -189,9 +189,12 @@ __global__ void __launch_bounds__(kThreads, 6) rope_kernel(const __grid_constant
       for (int o = LANES / 2; o > 0; o >>= 1)
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) sum[u] += __shfl_xor_sync(0xffffffffu, sum[u], o, LANES);
+      // (L2: a comparison, not fminf, which would turn the NaN of a row with one into 1 / eps)
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u)
-        f[u] *= p.norm == HACK_NORM_RMS ? rsqrtf(fmaf(sum[u], 1.f / D, p.eps)) : fminf(rsqrtf(sum[u]), p.inv_eps);
+      for (int u = 0; u < kUnroll; ++u) {
+        const float r = rsqrtf(p.norm == HACK_NORM_RMS ? fmaf(sum[u], 1.f / D, p.eps) : sum[u]);
+        f[u] *= p.norm == HACK_NORM_L2 && r > p.inv_eps ? p.inv_eps : r;
+      }
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {

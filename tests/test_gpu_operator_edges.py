@@ -1,0 +1,58 @@
+"""Values and sizes at the edges of the operators around the cache, against their definitions in 64 bits."""
+import pytest
+import torch
+
+from tests import rope_reference as rope_ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def hb():
+    import __graft_entry__ as ge
+    ge.build()
+    import paper_2504_09261_b200 as pkg
+    return pkg
+
+
+def _gen(seed):
+    return torch.Generator("cuda").manual_seed(seed)
+
+
+def _ints(*x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+# ------------------------------------------------------------------ norms and rotation
+def _same_numbers(out, want, size):
+    """NaN where the definition has NaN, the same infinities, and everything else within the bound of roundings."""
+    out, finite = out.double(), torch.isfinite(want)
+    assert torch.equal(torch.isnan(out), torch.isnan(want))
+    infinite = torch.isinf(want)
+    assert torch.equal(out[infinite], want[infinite])
+    return ((out - want).abs() - size)[finite]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("norm", [0, 1, 2])
+@pytest.mark.parametrize("dim,rotary,layout", [(128, 128, 0), (64, 32, 1), (64, 20, 0), (128, 0, 0)])
+def test_rows_with_no_numbers_and_infinities(hb, dtype, norm, dim, rotary, layout):
+    """A NaN or an infinity in a row is in the result what the definition makes of it, and the rows beside it do not see it."""
+    g = _gen(dim + norm)
+    b, h, n = 2, 5, 9
+    x = torch.randn(b, h, n, dim, generator=g, device="cuda").to(dtype)
+    x[0, 1, 3, 5] = float("nan")
+    x[0, 2, 4, dim - 1] = float("nan")
+    x[1, 0, 0, 7] = float("inf")
+    x[1, 4, 8, 0] = -float("inf")
+    x[1, 3, 2] = 0                                           # a row without length beside them
+    out = torch.empty_like(x)
+    weight = 1 + 0.3 * torch.rand(dim, generator=g, device="cuda")
+    pos = torch.arange(n, dtype=torch.int32, device="cuda") + 3
+    plan = hb.hack_rope_plan(dim, rotary, layout=layout) if rotary else None
+    hb.hack_qk_norm_rope(plan, x, None, None, out, None, None, pos if rotary else None, norm=norm, eps=1e-6, q_weight=weight)
+    want = rope_ref.normalise(x, norm, 1e-6, weight)
+    size = want.abs()
+    if rotary:
+        want, size = rope_ref.rotate(want, pos, rotary, layout, 1, *rope_ref.frequencies(rotary, 1))
+    assert _same_numbers(out, want, rope_ref.bound(want, size, dtype)).max() <= 0
