@@ -338,7 +338,7 @@ HACK_API hack_status_t hack_rope(const hack_rope_plan_t* plan, const hack_rope_a
 
 enum { HACK_NORM_NONE = 0,
        HACK_NORM_RMS = 1,     /* x / sqrt(mean x^2 + eps) */
-       HACK_NORM_L2 = 2 };    /* x / max(|x|, eps) */
+       HACK_NORM_L2 = 2 };    /* x / max(|x|, eps); eps is one whose fp32 reciprocal is finite */
 typedef struct {
   int32_t device, dtype, batch, n_heads, n_kv_heads, n_tokens, head_dim;
   int32_t norm;               /* HACK_NORM_*, of every row of q and k on its own */

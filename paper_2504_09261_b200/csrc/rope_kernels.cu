@@ -407,6 +407,8 @@ extern "C" hack_status_t hack_qk_norm_rope(const hack_rope_plan_t* plan, const h
   if ((k || v) && a.n_kv_heads < 1) { set_error("n_kv_heads must be positive"); return HACK_ERR_INVALID_ARG; }
   if (a.norm < HACK_NORM_NONE || a.norm > HACK_NORM_L2) { set_error("unknown norm"); return HACK_ERR_INVALID_ARG; }
   if (a.norm != HACK_NORM_NONE && !(a.eps > 0.f && std::isfinite(a.eps))) { set_error("eps must be finite and positive"); return HACK_ERR_INVALID_ARG; }
+  // (a row without length is multiplied by it)
+  if (a.norm == HACK_NORM_L2 && !std::isfinite(1.f / a.eps)) { set_error("the L2 norm needs an eps whose reciprocal is finite"); return HACK_ERR_INVALID_ARG; }
   if (!plan != !positions) { set_error("plan and positions: both or neither"); return HACK_ERR_INVALID_ARG; }
   if (plan && bad_plan(plan, a.head_dim)) return HACK_ERR_INVALID_ARG;
   if (a.n_tokens == 0) return HACK_OK;
