@@ -679,6 +679,8 @@ extern "C" hack_status_t hack_kv4_workspace(const hack_kv4_t* kv, const hack_kv4
   const hack_status_t s = check_attend(kv, args);
   if (s != HACK_OK) return s;
   if (!bytes) return invalid("bytes is NULL");
+  *bytes = 0;
+  if (args->n_queries == 0) return HACK_OK;      // (there is nothing to plan a launch for)
   HACK_ON_DEVICE_OF(kv->device);
   Kv4AttendParams p{};
   return plan(kv, args, p, *bytes);

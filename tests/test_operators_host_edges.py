@@ -19,3 +19,28 @@ def test_an_eps_without_a_reciprocal_is_refused(hb, norm, eps, refused):
     args = bd.HackQkvArgs(0, 0, 1, 2, 0, 0, 64, norm, eps, 0, 0, *([none] * 6))       # (no tokens: nothing else is looked at)
     assert bd.lib.hack_qk_norm_rope(None, C.addressof(args), *([None] * 12)) == (1 if refused else 0)
     assert not refused or "reciprocal" in hb.hack_last_error()
+
+
+def _kv4(**change):
+    from paper_2504_09261_b200 import binding as bd
+    f = dict(device=0, batch=2, n_kv_heads=3, head_dim=128, cap=50, reserved=0, rows=300, row_off=None, k_codes=4096, v_codes=8192, k_scales=12288,
+             v_scales=16384)
+    f.update(change)
+    return bd.HackKv4Planes(*f.values())
+
+
+def _attend(**change):
+    from paper_2504_09261_b200 import binding as bd
+    f = dict(dtype=1, n_heads=6, n_queries=1, max_len=10, appended=0, causal=0, window=0, n_sink=0, sm_scale=0.0, wait_polls=0, workspace_bytes=0)
+    form = change.pop("form", 0)
+    f.update(change)
+    return bd.HackKv4Attend(*f.values(), bd.HackStrides(768, 128, 128), bd.HackStrides(768, 128, 128), form, 0)
+
+
+@pytest.mark.parametrize("form", [0, 1, 2])
+def test_no_queries_need_no_workspace(hb, form):
+    """(A launch of no tiles cannot be planned: the share of the multiprocessors for each would be a division by zero.)"""
+    from paper_2504_09261_b200 import binding as bd
+    need = C.c_size_t(77)
+    assert bd.lib.hack_kv4_workspace(C.addressof(_kv4()), C.addressof(_attend(n_queries=0, form=form)), C.byref(need)) == 0
+    assert need.value == 0
