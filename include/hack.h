@@ -387,7 +387,7 @@ HACK_API hack_status_t hack_scale_step_qkv(hack_cache_t* cache, int32_t layer, i
  * ---------------------------------------------------------------------------------------------- */
 typedef struct {
   int32_t device, batch, n_kv_heads, head_dim;   /* head_dim 64 or 128 */
-  int32_t cap, reserved;
+  int32_t cap, reserved;                         /* cap: at most 2^31 - 512 */
   int64_t rows;                                  /* of each plane */
   const int64_t* row_off;
   void *k_codes, *v_codes, *k_scales, *v_scales;

@@ -17,6 +17,7 @@ namespace {
 using namespace kv4;
 
 constexpr int kThreads = 256;
+constexpr int kMaxCap = 0x7fffffff - 511;
 
 struct RowsParams {
   Planes planes;
@@ -312,6 +313,8 @@ hack_status_t kv4_check(const hack_kv4_t* kv) {
   if (kv->head_dim != 64 && kv->head_dim != 128) { set_error("head_dim must be 64 or 128"); return HACK_ERR_UNSUPPORTED; }
   if (kv->device < 0 || kv->batch < 1 || kv->n_kv_heads < 1 || kv->cap < 1 || (long long)kv->batch * kv->n_kv_heads > 0x7fffffffll)
     return invalid("batch, n_kv_heads and cap must be positive, device not negative");
+  // (a tile of 128 rows that starts among a head's last ones must end within 32 bits)
+  if (kv->cap > kMaxCap) return invalid("cap is beyond 2^31 - 512 rows");
   if (kv->rows < kv->cap || (!kv->row_off && kv->rows < (long long)kv->batch * kv->n_kv_heads * kv->cap)) return invalid("the planes have too few rows");
   const void* planes[4] = {kv->k_codes, kv->v_codes, kv->k_scales, kv->v_scales};
   for (const void* q : planes)

@@ -44,3 +44,17 @@ def test_no_queries_need_no_workspace(hb, form):
     need = C.c_size_t(77)
     assert bd.lib.hack_kv4_workspace(C.addressof(_kv4()), C.addressof(_attend(n_queries=0, form=form)), C.byref(need)) == 0
     assert need.value == 0
+
+
+@pytest.mark.parametrize("cap,refused", [(2 ** 31 - 1, True), (2 ** 31 - 511, True), (2 ** 31 - 512, False)])
+def test_a_cap_next_to_the_end_of_32_bits_is_refused(hb, cap, refused):
+    """A run of rows that starts in front of such a length would end past 32 bits and be taken for one that lies within it."""
+    from paper_2504_09261_b200 import binding as bd
+    kv, at, need = _kv4(cap=cap, rows=6 * 2 ** 31), _attend(n_queries=0), C.c_size_t()
+    k = C.addressof(kv)
+    rows = bd.HackKv4Rows(1, 0)
+    want = 1 if refused else 0
+    assert bd.lib.hack_kv4_workspace(k, C.addressof(at), C.byref(need)) == want
+    assert bd.lib.hack_kv4_attend(k, C.addressof(at), None, None, None, None, None, None) == want
+    assert bd.lib.hack_kv4_append(k, C.addressof(rows), None, None, None, None, None) == want
+    assert bd.lib.hack_kv4_read(k, C.addressof(rows), None, None, None, None) == want
