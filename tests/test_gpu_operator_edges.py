@@ -56,3 +56,18 @@ def test_rows_with_no_numbers_and_infinities(hb, dtype, norm, dim, rotary, layou
     if rotary:
         want, size = rope_ref.rotate(want, pos, rotary, layout, 1, *rope_ref.frequencies(rotary, 1))
     assert _same_numbers(out, want, rope_ref.bound(want, size, dtype)).max() <= 0
+
+
+# ------------------------------------------------------------------ attention over 4 bits
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("dim,kv_heads,group,tokens,length", [(64, 32, 1, 1, 4096), (64, 32, 7, 1, 4096), (64, 16, 13, 1, 3000), (64, 2, 3, 5, 900),
+                                                              (128, 32, 1, 1, 4096), (128, 3, 5, 3, 1000)])
+def test_clusters_whose_warps_have_rows_for_some_of_their_threads(hb, dtype, dim, kv_heads, group, tokens, length):
+    """At head_dim 64 half a warp adds up a row: with an odd number of rows the other half is done first."""
+    from tests.test_gpu_kv4 import Planes, _check
+    kv4 = Planes(1, dim)
+    kv4 = hb.HackKv4(*(t.expand(kv_heads * length, -1).contiguous() for t in kv4.all()), batch=1, n_kv_heads=kv_heads, cap=length)
+    q = torch.empty(1, kv_heads * group, tokens, dim, dtype=dtype, device="cuda")
+    # no workspace: one launch, in clusters (a single CTA for so many rows takes two to three times as long as a few)
+    assert kv4.hack_kv4_workspace(q, length) == 0
+    _check(hb, _gen(group), dtype, dim, 1, kv_heads, group, tokens, length, [length] + [length * i // kv_heads for i in range(1, kv_heads)])
