@@ -447,6 +447,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid
 #pragma unroll 1
       for (int half = 0; half < D / 64; ++half) {
         uint32_t o[64];
+        __syncwarp();                                              // (threads without a row of their own left the half before early)
         if (nblk > 0) {
           tmem_ld32(o_addr + half * 64, o);
           tmem_ld32(o_addr + half * 64 + 32, o + 32);
@@ -597,6 +598,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv4_attend_tc_kernel(const __grid
       drained(&bars->drain[1]);
     }
   }
+  __syncwarp();                              // (an issuer is one thread of its warp)
   tc_fence_before();
   __syncthreads();
   if (warp == kQkWarp) {

@@ -71,3 +71,11 @@ def test_clusters_whose_warps_have_rows_for_some_of_their_threads(hb, dtype, dim
     # no workspace: one launch, in clusters (a single CTA for so many rows takes two to three times as long as a few)
     assert kv4.hack_kv4_workspace(q, length) == 0
     _check(hb, _gen(group), dtype, dim, 1, kv_heads, group, tokens, length, [length] + [length * i // kv_heads for i in range(1, kv_heads)])
+
+
+@pytest.mark.parametrize("kv_heads,group,tokens,cap", [(1, 1, 129, 300), (2, 3, 43, 1500), (1, 1, 1, 700), (150, 1, 255, 131)])
+def test_tiles_whose_warps_have_rows_for_some_of_their_threads(hb, kv_heads, group, tokens, cap):
+    """Tiles of 128 query rows of which one, 127 or a few in a warp are there, head_dim 128 (the output leaves in two halves), with the
+    blocks of a unit on one CTA and shared."""
+    from tests.test_gpu_kv4 import _check
+    _check(hb, _gen(cap), torch.bfloat16, 128, 1, kv_heads, group, tokens, cap, [cap] + [cap * i // kv_heads for i in range(1, kv_heads)], form=2)
