@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import importlib.util
+import operator
 import os
 import sysconfig
 from typing import Optional, Sequence
@@ -301,6 +302,16 @@ def _keep(key, args):
     _args_of[key] = (args, C.addressof(args))
 
 
+def _first(head, make, address, lead, stream, *tensors):
+    """A call that found no struct.  head holds plain numbers by now: a tensor of one element, say, would be held by its identity,
+    and found again with another value in it."""
+    status = _run(_args_of, head, address, lead, stream, *tensors)
+    if status.__class__ is tuple:
+        _keep(status, make())
+        status = _run(_args_of, head, address, lead, stream, *tensors)
+    return status
+
+
 def hack_rope_plan(head_dim: int, rotary_dim: Optional[int] = None, layout: int = HACK_ROPE_HALF, axes: int = 1,
                    base: float = 10000.0, scaling: int = HACK_ROPE_PLAIN, factor: float = 1.0, trained_length: int = 0,
                    turns_fast: float = 0.0, turns_slow: float = 0.0) -> HackRopePlan:
@@ -316,8 +327,9 @@ def hack_rope(plan: HackRopePlan, x, y, positions, transpose: bool = False, stre
     head = ("rope", plan.axes, plan.head_dim, transpose)
     status = _run(_args_of, head, _ROPE, C.addressof(plan), stream, x, y, positions)
     if status.__class__ is tuple:
-        _keep(status, _rope_args(plan, x, y, positions, transpose))
-        status = _run(_args_of, head, _ROPE, C.addressof(plan), stream, x, y, positions)
+        transpose = bool(transpose)
+        status = _first(("rope", plan.axes, plan.head_dim, transpose), lambda: _rope_args(plan, x, y, positions, transpose), _ROPE,
+                        C.addressof(plan), stream, x, y, positions)
     if status:
         _check(status)
 
@@ -357,12 +369,15 @@ def hack_qk_norm_rope(plan: Optional[HackRopePlan], q, k, v, q_out, k_out, v_out
                       eps: float = 1e-6, q_weight=None, k_weight=None, q_gain=None, k_gain=None, stream=None) -> None:
     """Queries and keys normalised per head, weighted and rotated, values copied: from views of a projection's output to the
     layout of the steps.  All tensors [batch, heads, tokens, head_dim]; plan and positions None: no rotation."""
-    head = ("qkv", None if plan is None else (plan.axes, plan.head_dim), norm, eps)
+    of_plan = None if plan is None else (plan.axes, plan.head_dim)
     lead = None if plan is None else C.addressof(plan)
-    status = _run(_args_of, head, _QK_NORM_ROPE, lead, stream, q, k, v, q_out, k_out, v_out, positions, q_weight, k_weight, q_gain, k_gain)
+    status = _run(_args_of, ("qkv", of_plan, norm, eps), _QK_NORM_ROPE, lead, stream, q, k, v, q_out, k_out, v_out, positions, q_weight, k_weight,
+                  q_gain, k_gain)
     if status.__class__ is tuple:
-        _keep(status, _qkv_args(plan, q, k, v, q_out, k_out, v_out, positions, norm, eps, q_weight, k_weight, q_gain, k_gain))
-        status = _run(_args_of, head, _QK_NORM_ROPE, lead, stream, q, k, v, q_out, k_out, v_out, positions, q_weight, k_weight, q_gain, k_gain)
+        norm, eps = operator.index(norm), float(eps)
+        status = _first(("qkv", of_plan, norm, eps),
+                        lambda: _qkv_args(plan, q, k, v, q_out, k_out, v_out, positions, norm, eps, q_weight, k_weight, q_gain, k_gain),
+                        _QK_NORM_ROPE, lead, stream, q, k, v, q_out, k_out, v_out, positions, q_weight, k_weight, q_gain, k_gain)
     if status:
         _check(status)
 
@@ -375,6 +390,7 @@ class HackKv4:
     def __init__(self, k_codes, k_scales, v_codes, v_scales, batch: int, n_kv_heads: int, cap: int, row_off=None):
         dim = 2 * k_codes.shape[-1]
         rows = k_codes.shape[0]
+        batch, n_kv_heads, cap = map(operator.index, (batch, n_kv_heads, cap))
         for t, width in ((k_codes, dim // 2), (v_codes, dim // 2), (k_scales, dim // 16), (v_scales, dim // 16)):
             if str(t.dtype) != "torch.uint8" or tuple(t.shape) != (rows, width) or not t.is_contiguous() or \
                     t.get_device() != k_codes.get_device():
@@ -408,16 +424,14 @@ class HackKv4:
     def hack_kv4_append(self, k, v, lens, new_lens=None, stream=None) -> None:
         status = _run(_args_of, self._head, _KV4_APPEND, self._address, stream, k, v, lens, new_lens)
         if status.__class__ is tuple:
-            _keep(status, self._rows(k, v, lens, new_lens))
-            status = _run(_args_of, self._head, _KV4_APPEND, self._address, stream, k, v, lens, new_lens)
+            status = _first(self._head, lambda: self._rows(k, v, lens, new_lens), _KV4_APPEND, self._address, stream, k, v, lens, new_lens)
         if status:
             _check(status)
 
     def hack_kv4_read(self, k_out, v_out, first, stream=None) -> None:
         status = _run(_args_of, self._head, _KV4_READ, self._address, stream, k_out, v_out, first)
         if status.__class__ is tuple:
-            _keep(status, self._rows(k_out, v_out, first, None))
-            status = _run(_args_of, self._head, _KV4_READ, self._address, stream, k_out, v_out, first)
+            status = _first(self._head, lambda: self._rows(k_out, v_out, first, None), _KV4_READ, self._address, stream, k_out, v_out, first)
         if status:
             _check(status)
 
@@ -450,8 +464,11 @@ class HackKv4:
             room = 0 if workspace is None else workspace.numel() * workspace.element_size()
             if room and (not workspace.is_contiguous() or workspace.get_device() != self.device):
                 raise ValueError("the workspace must be contiguous and on the cache's device")
-            _keep(status, self._attend(q, out, lens, max_len, new_lens, appended, causal, n_sink, window, sm_scale, room, form))
-            status = _run(_args_of, head, _KV4_ATTEND, self._address, stream, q, out, lens, new_lens, workspace)
+            max_len, n_sink, window, form = map(operator.index, (max_len, n_sink, window, form))
+            appended, causal, sm_scale = bool(appended), bool(causal), float(sm_scale)
+            status = _first((self._head, max_len, appended, causal, n_sink, window, sm_scale, form),
+                            lambda: self._attend(q, out, lens, max_len, new_lens, appended, causal, n_sink, window, sm_scale, room, form),
+                            _KV4_ATTEND, self._address, stream, q, out, lens, new_lens, workspace)
         if status:
             _check(status)
 

@@ -58,3 +58,51 @@ def test_a_cap_next_to_the_end_of_32_bits_is_refused(hb, cap, refused):
     assert bd.lib.hack_kv4_attend(k, C.addressof(at), None, None, None, None, None, None) == want
     assert bd.lib.hack_kv4_append(k, C.addressof(rows), None, None, None, None, None) == want
     assert bd.lib.hack_kv4_read(k, C.addressof(rows), None, None, None, None) == want
+
+
+@pytest.fixture
+def store(monkeypatch):
+    """The binding's argument structs, empty.  (Calls on CPU tensors are marshalled as any other and refused by the library.)"""
+    from paper_2504_09261_b200 import binding as bd
+    held = {}
+    monkeypatch.setattr(bd, "_args_of", held)
+    return held
+
+
+def _cpu_cache(hb):
+    import torch
+    return hb.HackKv4(*(torch.zeros(50, n, dtype=torch.uint8) for n in (32, 4, 32, 4)), batch=1, n_kv_heads=1, cap=50)
+
+
+def test_arguments_are_held_by_value(hb, store):
+    """A number that lives in a tensor and changes there: the call sees what is in it, not what was."""
+    import torch
+    x, lens = torch.zeros(1, 1, 1, 64), torch.zeros(1, dtype=torch.int32)
+    kv4 = _cpu_cache(hb)
+    numbers = dict(max_len=torch.tensor(10), n_sink=torch.tensor(1), window=torch.tensor(4), form=torch.tensor(0), causal=torch.tensor(False),
+                   appended=torch.tensor(False), sm_scale=torch.tensor(0.5))
+    eps, norm, transpose = torch.tensor(0.5), torch.tensor(1), torch.tensor(False)
+    plan = hb.hack_rope_plan(64)
+
+    def newest(call):
+        with pytest.raises(hb.HackError) as e:
+            call()
+        assert e.value.status == 1
+        return list(store.values())[-1][0]
+
+    def calls():
+        a = newest(lambda: kv4.hack_kv4_attend(x, x.clone(), lens, **numbers))
+        n = newest(lambda: hb.hack_qk_norm_rope(None, x, None, None, x, None, None, None, norm=norm, eps=eps))
+        r = newest(lambda: hb.hack_rope(plan, x, x, lens, transpose=transpose))
+        return a.max_len, a.n_sink, a.window, a.form, a.causal, a.appended, a.sm_scale, n.eps, n.norm, r.transpose
+
+    assert calls() == (10, 1, 4, 0, 0, 0, 0.5, 0.5, 1, 0)
+    for t in (*numbers.values(), eps, norm, transpose):
+        t.add_(1) if t.dtype != torch.bool else t.fill_(True)
+    assert calls() == (11, 2, 5, 1, 1, 1, 1.5, 1.5, 2, 1)
+    held = len(store)
+    with pytest.raises(hb.HackError):
+        kv4.hack_kv4_attend(x, x.clone(), lens, **numbers)
+    assert held == 6 and len(store) == held                              # a value that was seen before needs no other struct
+    for key in store:
+        assert all(isinstance(v, (str, int, float, bool, tuple, type(None))) for v in key[0]), key[0]
