@@ -305,11 +305,11 @@ def _keep(key, args):
 def _first(head, make, address, lead, stream, *tensors):
     """A call that found no struct.  head holds plain numbers by now: a tensor of one element, say, would be held by its identity,
     and found again with another value in it."""
-    status = _run(_args_of, head, address, lead, stream, *tensors)
-    if status.__class__ is tuple:
-        _keep(status, make())
+    while True:                       # (another thread may empty the store between the two lines below)
         status = _run(_args_of, head, address, lead, stream, *tensors)
-    return status
+        if status.__class__ is not tuple:
+            return status
+        _keep(status, make())
 
 
 def hack_rope_plan(head_dim: int, rotary_dim: Optional[int] = None, layout: int = HACK_ROPE_HALF, axes: int = 1,

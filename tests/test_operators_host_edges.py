@@ -106,3 +106,30 @@ def test_arguments_are_held_by_value(hb, store):
     assert held == 6 and len(store) == held                              # a value that was seen before needs no other struct
     for key in store:
         assert all(isinstance(v, (str, int, float, bool, tuple, type(None))) for v in key[0]), key[0]
+
+
+def test_a_store_that_is_emptied_meanwhile(hb, store, monkeypatch):
+    """Another thread's call empties the full store between this one's struct and its use: the struct is made again."""
+    import torch
+    from paper_2504_09261_b200 import binding as bd
+    keep, made = bd._keep, []
+
+    def meanwhile(key, args):
+        keep(key, args)
+        made.append(key)
+        if len(made) % 2:
+            store.clear()
+
+    monkeypatch.setattr(bd, "_keep", meanwhile)
+    x, ints = torch.zeros(1, 1, 1, 64), torch.zeros(1, dtype=torch.int32)
+    kv4 = _cpu_cache(hb)
+    plan = hb.hack_rope_plan(64)
+    calls = (lambda: hb.hack_rope(plan, x, x, ints), lambda: hb.hack_qk_norm_rope(None, x, None, None, x, None, None, None),
+             lambda: kv4.hack_kv4_append(x, x, ints), lambda: kv4.hack_kv4_read(x, x.clone(), ints[:1]),
+             lambda: kv4.hack_kv4_attend(x, x, ints, 10))
+    for i, call in enumerate(calls):
+        store.clear()
+        with pytest.raises(hb.HackError) as e:
+            call()
+        assert e.value.status == 1                                       # (the library's answer to tensors on the host)
+        assert len(made) == 2 * (i + 1)
