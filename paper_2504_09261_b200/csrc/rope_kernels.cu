@@ -358,7 +358,8 @@ extern "C" hack_status_t hack_rope_plan(int32_t head_dim, int32_t rotary_dim, in
     double f = std::pow(b, -2.0 * i / dim);
     if (scaling == HACK_ROPE_LINEAR) f /= factor;
     if (scaling == HACK_ROPE_BANDS) {
-      const double ramp = std::min(1.0, std::max(0.0, (i - low) / std::max(high - low, 0.001)));
+      // (from `high` on by itself: where every pair turns less than turns_slow times, high is 0 or below and there is no ramp)
+      const double ramp = i >= high ? 1.0 : std::min(1.0, std::max(0.0, (i - low) / std::max(high - low, 0.001)));
       f = f * (1.0 - ramp) + f / factor * ramp;
     }
     for (int a = 0; a < axes; ++a) p.freq[a * pairs + i] = f;

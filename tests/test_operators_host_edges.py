@@ -133,3 +133,25 @@ def test_a_store_that_is_emptied_meanwhile(hb, store, monkeypatch):
             call()
         assert e.value.status == 1                                       # (the library's answer to tensors on the host)
         assert len(made) == 2 * (i + 1)
+
+
+@pytest.mark.parametrize("dim,axes,trained,fast,slow", [
+    (64, 1, 512, 200.0, 100.0),          # every pair turns less than turns_slow times
+    (64, 1, 4, 32.0, 1.0), (128, 2, 6, 0.0, 0.0), (128, 1, 512, 81.0, 80.0), (64, 2, 1, 2.0, 1.0),
+    (64, 1, 4096, 32.0, 1.0), (128, 1, 10 ** 9, 32.0, 1.0), (128, 2, 8192, 1000.0, 0.5), (64, 1, 512, 80.0, 20.0)])
+def test_bands_stretch_what_turns_too_little(hb, dim, axes, trained, fast, slow):
+    """Pairs that turn at least turns_fast times keep their frequency, pairs that turn turns_slow times or less have it divided."""
+    import math
+    factor = 8.0
+    plan = hb.hack_rope_plan(dim, axes=axes, scaling=hb.HACK_ROPE_BANDS, factor=factor, trained_length=trained, turns_fast=fast, turns_slow=slow)
+    plain = hb.hack_rope_plan(dim, axes=axes)
+    fast, slow = fast or 32.0, slow or 1.0
+    last = 1.0
+    for i in range(dim // 2 // axes):
+        part, turns = plan.freq[i] / plain.freq[i], trained * plain.freq[i] / (2 * math.pi)
+        if turns < slow * (1 - 1e-9):
+            assert abs(part * factor - 1) < 1e-12, (i, turns)
+        if turns > fast * (1 + 1e-9):
+            assert part == 1, (i, turns)
+        assert 1 / factor * (1 - 1e-12) <= part <= last                # and a ramp downwards between them
+        last = part
