@@ -1022,9 +1022,7 @@ hack_status_t hack_store_kv4(hack_cache_t* c, int32_t layer, const hack_kv4_t* k
   hack_step_info_t p{};
   p.kept_s = ls.len[0];
   p.kept_c = ls.len[1];
-  const hack_status_t r = hack::launch_store_kv4(make_args(c, layer, 0, p), c->cfg.dtype, kv, lens, (cudaStream_t)stream);
-  if (r == HACK_OK) ++c->launches;
-  return r;
+  return hack::launch_store_kv4(make_args(c, layer, 0, p), c->cfg.dtype, kv, lens, c->launches, (cudaStream_t)stream);
 }
 
 hack_status_t hack_get_lengths(const hack_cache_t* c, int32_t layer, int32_t* host_out) {

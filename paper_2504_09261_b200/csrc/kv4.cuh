@@ -64,7 +64,7 @@ __device__ __forceinline__ void add_bf162(float& x, float& y, uint32_t w) {
 
 hack_status_t kv4_check(const hack_kv4_t* kv);          // HACK_OK, or the error with its text
 kv4::Planes kv4_planes(const hack_kv4_t* kv);
-// The rows that a layer holds (a: its lengths and planes) behind the lens rows of the 4-bit cache.
-hack_status_t launch_store_kv4(const StepArgs& a, int dtype, const hack_kv4_t* kv, const int32_t* lens, cudaStream_t st);
+// The rows that a layer holds (a: its lengths and planes) behind the lens rows of the 4-bit cache; launches: counts on.
+hack_status_t launch_store_kv4(const StepArgs& a, int dtype, const hack_kv4_t* kv, const int32_t* lens, uint64_t& launches, cudaStream_t st);
 
 }  // namespace hack

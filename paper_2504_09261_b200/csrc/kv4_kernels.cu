@@ -327,7 +327,7 @@ kv4::Planes kv4_planes(const hack_kv4_t* kv) {
           static_cast<unsigned char*>(kv->k_scales), static_cast<unsigned char*>(kv->v_scales), kv->row_off, (long long)kv->rows, kv->cap};
 }
 
-hack_status_t launch_store_kv4(const StepArgs& a, int dtype, const hack_kv4_t* kv, const int32_t* lens, cudaStream_t st) {
+hack_status_t launch_store_kv4(const StepArgs& a, int dtype, const hack_kv4_t* kv, const int32_t* lens, uint64_t& launches, cudaStream_t st) {
   RowsParams p = rows_params(kv);
   p.k = a.k_plane;
   p.v = a.v_plane;
@@ -341,7 +341,9 @@ hack_status_t launch_store_kv4(const StepArgs& a, int dtype, const hack_kv4_t* k
   }
   p.n_tokens = longest;
   if (longest == 0) return HACK_OK;
-  return launch_rows(false, p, dtype, a.head_dim, a.batch * a.n_heads, st);
+  const hack_status_t s = launch_rows(false, p, dtype, a.head_dim, a.batch * a.n_heads, st);
+  launches += s == HACK_OK;
+  return s;
 }
 
 }  // namespace hack

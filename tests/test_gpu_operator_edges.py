@@ -79,3 +79,25 @@ def test_tiles_whose_warps_have_rows_for_some_of_their_threads(hb, kv_heads, gro
     blocks of a unit on one CTA and shared."""
     from tests.test_gpu_kv4 import _check
     _check(hb, _gen(cap), torch.bfloat16, 128, 1, kv_heads, group, tokens, cap, [cap] + [cap * i // kv_heads for i in range(1, kv_heads)], form=2)
+
+
+# ------------------------------------------------------------------ a layer's rows
+def test_launches_are_counted_as_they_are_made(hb):
+    from tests.parity_util import make_cache
+    from tests.test_gpu_kv4 import Planes
+    from workloads import SyntheticQKV, get_config
+    cfg = get_config(1, n_layers=1)
+    cache = make_cache(cfg, SyntheticQKV(cfg).head_is_contextual.numpy())
+    b, h, d = cfg.batch, cfg.n_heads, cfg.head_dim
+    planes = Planes(b * h * 4, d)
+    kv4, lens = planes.handle(hb, b, h, 4), torch.zeros(b * h, dtype=torch.int32, device="cuda")
+    cache.hack_store_kv4(0, kv4, lens)                       # a layer without rows: nothing to launch
+    assert cache.hack_launch_count() == 0
+    assert all((p == 0x5a).all() for p in planes.all())
+    q = torch.randn(b, h, 1, d, generator=_gen(2), device="cuda").to(torch.bfloat16)
+    out, pos = torch.empty_like(q), _ints(0)
+    cache.hack_scale_step_qkv(0, 0, hb.hack_rope_plan(d), q, q, q, out, pos)
+    steps = cache.hack_launch_count()
+    cache.hack_store_kv4(0, kv4, lens)
+    assert steps >= 2 and cache.hack_launch_count() == steps + 1
+    cache.close()
