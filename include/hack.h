@@ -292,7 +292,8 @@ HACK_API hack_status_t hack_debug_check(hack_cache_t* cache, int32_t* violations
  * Every row starts on a 16-byte boundary (base address and strides).  head_dim is 64 or 128, dtype
  * HACK_F32 or HACK_BF16; sums and products are fp32, rounded once.  Nothing is allocated or kept.
  * An output may be its input (same address, same strides); other overlaps are not allowed.
- * A call with no tokens does nothing.  `device` is made current for the call.
+ * A call with no tokens does nothing.  `device` is made current for the call.  Arrays of numbers (positions,
+ * weights, gains, lengths) start on a multiple of their elements' size.
  * ---------------------------------------------------------------------------------------------- */
 typedef struct { int64_t batch, head, token; } hack_strides_t;   /* in elements */
 

@@ -44,6 +44,9 @@ inline const char* view_error(const void* ptr, const hack_strides_t& s, int batc
   return nullptr;
 }
 
+// Whether an array of `elt`-byte numbers (or NULL) starts off their size: the kernels read them one by one.
+inline bool off_its_size(const void* ptr, int elt) { return reinterpret_cast<uintptr_t>(ptr) % elt != 0; }
+
 }  // namespace hack
 
 #define HACK_ON_DEVICE_OF(device)                                                                     \

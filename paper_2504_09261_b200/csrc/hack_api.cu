@@ -1016,7 +1016,7 @@ hack_status_t hack_store_kv4(hack_cache_t* c, int32_t layer, const hack_kv4_t* k
   if (s != HACK_OK) return s;
   if (kv->batch != c->cfg.batch || kv->n_kv_heads != c->cfg.n_heads || kv->head_dim != c->cfg.head_dim || kv->device != c->cfg.device)
     return fail(HACK_ERR_INVALID_ARG, "the 4-bit cache has another batch, heads, head_dim or device");
-  if (!lens) return fail(HACK_ERR_INVALID_ARG, "lens is NULL");
+  if (!lens || hack::off_its_size(lens, 4)) return fail(HACK_ERR_INVALID_ARG, "lens is NULL or not on a multiple of 4 bytes");
   HACK_ON_DEVICE(c);
   const LayerState& ls = c->layers[layer];
   hack_step_info_t p{};

@@ -695,7 +695,7 @@ extern "C" hack_status_t hack_kv4_attend(const hack_kv4_t* kv, const hack_kv4_at
   if (s != HACK_OK) return s;
   const hack_kv4_attend_t& a = *args;
   if (a.n_queries == 0) return HACK_OK;
-  if (!lens) return invalid("lens is NULL");
+  if (!lens || off_its_size(lens, 4) || off_its_size(new_lens, 4)) return invalid("lens is NULL, or lens or new_lens not on a multiple of 4 bytes");
   const int elt = a.dtype == HACK_F32 ? 4 : 2;
   const char* text = view_error(q, a.q, kv->batch, a.n_heads, a.n_queries, kv->head_dim, elt, false);
   if (!text) text = view_error(out, a.out, kv->batch, a.n_heads, a.n_queries, kv->head_dim, elt, true);

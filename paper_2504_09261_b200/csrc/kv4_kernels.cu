@@ -293,6 +293,7 @@ hack_status_t check_rows(const hack_kv4_t* kv, const hack_kv4_rows_t* r, const v
   if (r->n_tokens < 0) return invalid("n_tokens is negative");
   if (r->n_tokens == 0) return HACK_OK;
   if (!k || !v || !at) return invalid("a tensor is NULL");
+  if (off_its_size(at, 4)) return invalid("lengths or first rows are not on a multiple of 4 bytes");
   const int elt = r->dtype == HACK_F32 ? 4 : 2;
   const char* text = view_error(k, r->k, kv->batch, kv->n_kv_heads, r->n_tokens, kv->head_dim, elt, written);
   if (!text) text = view_error(v, r->v, kv->batch, kv->n_kv_heads, r->n_tokens, kv->head_dim, elt, written);
@@ -319,6 +320,7 @@ hack_status_t kv4_check(const hack_kv4_t* kv) {
   const void* planes[4] = {kv->k_codes, kv->v_codes, kv->k_scales, kv->v_scales};
   for (const void* q : planes)
     if (!q || (reinterpret_cast<uintptr_t>(q) & 15)) return invalid("a plane is NULL or not 16-byte aligned");
+  if (off_its_size(kv->row_off, 8)) return invalid("row_off is not on a multiple of 8 bytes");
   return HACK_OK;
 }
 
@@ -353,6 +355,7 @@ extern "C" hack_status_t hack_kv4_append(const hack_kv4_t* kv, const hack_kv4_ro
   using namespace hack;
   const hack_status_t s = check_rows(kv, rows, k, v, lens, false);
   if (s != HACK_OK || rows->n_tokens == 0) return s;
+  if (off_its_size(new_lens, 4)) return invalid("new_lens is not on a multiple of 4 bytes");
   HACK_ON_DEVICE_OF(kv->device);
   RowsParams p = rows_params(kv);
   p.n_tokens = rows->n_tokens;

@@ -377,7 +377,7 @@ extern "C" hack_status_t hack_rope(const hack_rope_plan_t* plan, const hack_rope
   if (st != HACK_OK) return st;
   if (bad_plan(plan, plan->head_dim)) return HACK_ERR_INVALID_ARG;
   if (a.n_tokens == 0) return HACK_OK;
-  if (!positions) { set_error("positions is NULL"); return HACK_ERR_INVALID_ARG; }
+  if (!positions || off_its_size(positions, 4)) { set_error("positions is NULL or not on a multiple of 4 bytes"); return HACK_ERR_INVALID_ARG; }
   const int elt = a.dtype == HACK_F32 ? 4 : 2;
   if (bad_view(x, a.x, a.batch, a.n_heads, a.n_tokens, plan->head_dim, elt, false) ||
       bad_view(y, a.y, a.batch, a.n_heads, a.n_tokens, plan->head_dim, elt, true))
@@ -413,6 +413,8 @@ extern "C" hack_status_t hack_qk_norm_rope(const hack_rope_plan_t* plan, const h
   if (!plan != !positions) { set_error("plan and positions: both or neither"); return HACK_ERR_INVALID_ARG; }
   if (plan && bad_plan(plan, a.head_dim)) return HACK_ERR_INVALID_ARG;
   if (a.n_tokens == 0) return HACK_OK;
+  for (const void* x : {positions, (const void*)q_weight, (const void*)k_weight, (const void*)q_gain, (const void*)k_gain})
+    if (off_its_size(x, 4)) { set_error("positions, weights or gains are not on a multiple of 4 bytes"); return HACK_ERR_INVALID_ARG; }
   const int elt = a.dtype == HACK_F32 ? 4 : 2;
   const void* in[3] = {q, k, v};
   void* out[3] = {q_out, k_out, v_out};

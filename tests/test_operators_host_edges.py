@@ -41,8 +41,8 @@ def _attend(**change):
 def test_no_queries_need_no_workspace(hb, form):
     """(A launch of no tiles cannot be planned: the share of the multiprocessors for each would be a division by zero.)"""
     from paper_2504_09261_b200 import binding as bd
-    need = C.c_size_t(77)
-    assert bd.lib.hack_kv4_workspace(C.addressof(_kv4()), C.addressof(_attend(n_queries=0, form=form)), C.byref(need)) == 0
+    need, kv, at = C.c_size_t(77), _kv4(), _attend(n_queries=0, form=form)
+    assert bd.lib.hack_kv4_workspace(C.addressof(kv), C.addressof(at), C.byref(need)) == 0
     assert need.value == 0
 
 
@@ -155,3 +155,25 @@ def test_bands_stretch_what_turns_too_little(hb, dim, axes, trained, fast, slow)
             assert part == 1, (i, turns)
         assert 1 / factor * (1 - 1e-12) <= part <= last                # and a ramp downwards between them
         last = part
+
+
+def test_arrays_off_their_size_are_refused(hb):
+    """The kernels read these one number at a time: one that straddles its own size would be a misaligned address on the GPU."""
+    from paper_2504_09261_b200 import binding as bd
+    held = hb.hack_rope_plan(128)
+    plan, strides = C.addressof(held), bd.HackStrides(768, 384, 128)
+    rope = bd.HackRopeArgs(0, 0, 1, 2, 3, 0, 0, 0, 0, strides, strides)
+    assert bd.lib.hack_rope(plan, C.addressof(rope), 4096, 8192, 16386, None) == 1 and "4 bytes" in hb.hack_last_error()
+    qkv = bd.HackQkvArgs(0, 0, 1, 2, 2, 3, 128, 1, 1e-6, 0, 0, *([strides] * 6))
+    for off in range(5):                     # positions, q_weight, k_weight, q_gain, k_gain
+        arrays = [8192 + (2 if i == off else 0) for i in range(5)]
+        assert bd.lib.hack_qk_norm_rope(plan, C.addressof(qkv), *([4096] * 6), *arrays, None) == 1
+        assert "4 bytes" in hb.hack_last_error()
+    kv, kv_off, at = _kv4(), _kv4(row_off=4100), _attend()
+    rows = bd.HackKv4Rows(1, 4, bd.HackStrides(1536, 512, 128), bd.HackStrides(1536, 512, 128))
+    k, r, a = C.addressof(kv), C.addressof(rows), C.addressof(at)
+    for call in (lambda: bd.lib.hack_kv4_append(k, r, 4096, 4096, 4098, None, None), lambda: bd.lib.hack_kv4_append(k, r, 4096, 4096, 4096, 4097, None),
+                 lambda: bd.lib.hack_kv4_read(k, r, 4096, 4096, 4099, None), lambda: bd.lib.hack_kv4_attend(k, a, 4096, 8192, 4097, None, None, None),
+                 lambda: bd.lib.hack_kv4_attend(k, a, 4096, 8192, 4096, 4098, None, None)):
+        assert call() == 1 and "4 bytes" in hb.hack_last_error()
+    assert bd.lib.hack_kv4_append(C.addressof(kv_off), r, 4096, 4096, 4096, None, None) == 1 and "8 bytes" in hb.hack_last_error()
