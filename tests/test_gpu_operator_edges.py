@@ -101,3 +101,71 @@ def test_launches_are_counted_as_they_are_made(hb):
     cache.hack_store_kv4(0, kv4, lens)
     assert steps >= 2 and cache.hack_launch_count() == steps + 1
     cache.close()
+
+
+# ------------------------------------------------------------------ which form serves a call
+@pytest.mark.parametrize("dim,heads,tokens,cap,many", [(128, 16, 32, 10521, False), (128, 16, 64, 10521, True), (128, 64, 64, 2240, True),
+                                                       (64, 4, 64, 700, False), (128, 16, 1024, 64, True), (64, 256, 256, 680, True)])
+def test_the_form_that_was_faster(hb, dim, heads, tokens, cap, many):
+    """At sizes timed in both forms.  They add up in different orders, so that some of a call's many results differ in a bit: the
+    library's own choice has all the bits of one of them."""
+    from tests.test_gpu_kv4 import Planes
+    g = _gen(heads + tokens)
+    planes = Planes(heads * cap, dim)
+    planes.randomise(g)
+    kv4 = planes.handle(hb, 1, heads, cap)
+    q = torch.randn(1, heads, tokens, dim, generator=g, device="cuda").to(torch.bfloat16)
+    lens, outs = _ints(*([cap] * heads)), []
+    for form in (0, hb.HACK_KV4_FEW, hb.HACK_KV4_MANY):
+        work = torch.empty(kv4.hack_kv4_workspace(q, cap, form=form), dtype=torch.uint8, device="cuda")
+        outs.append(torch.empty_like(q))
+        kv4.hack_kv4_attend(q, outs[-1], lens, cap, workspace=work, form=form)
+    assert not torch.equal(outs[1], outs[2])
+    assert torch.equal(outs[0], outs[2 if many else 1])
+    kv4.hack_kv4_poll_status()
+
+
+# ------------------------------------------------------------------ queries that are no numbers
+@pytest.mark.parametrize("dtype,form", [(torch.float32, 1), (torch.bfloat16, 1), (torch.bfloat16, 2)])
+@pytest.mark.parametrize("dim,tokens,length", [(64, 5, 300), (128, 3, 1000), (64, 150, 200), (128, 140, 90)])
+def test_queries_with_no_numbers_and_infinities(hb, dtype, form, dim, tokens, length):
+    """A query with a NaN has NaN for its result, and zeros where it sees no row at all; the queries beside it, in the same tile and the
+    same warp, are what they would be without it."""
+    from tests import kv4_reference as ref
+    from tests.test_gpu_kv4 import Planes
+    g, group = _gen(tokens + dim), 2
+    planes = Planes(length, dim)
+    planes.randomise(g)
+    # no element of a key is 0: an infinity in a query gives logits of both signs, of which one is certain to be +inf
+    planes.k_codes[planes.k_codes & 15 == 8] += 1
+    planes.k_codes[planes.k_codes >> 4 == 8] += 16
+    kv4 = planes.handle(hb, 1, 1, length)
+    q = torch.randn(1, group, tokens, dim, generator=g, device="cuda").to(dtype)
+    q[0, 0, 1, 3], q[0, 1, tokens - 1, dim - 1], q[0, 1, 0, 5] = float("nan"), float("inf"), float("nan")
+    bad = torch.zeros(group, tokens, dtype=torch.bool, device="cuda")
+    bad[0, 1] = bad[1, tokens - 1] = bad[1, 0] = True
+    for causal, rows in ((False, length), (True, length), (True, tokens - 1)):      # the last: the first query of all sees nothing
+        rows = min(rows, length)
+        out = torch.full_like(q, 77.0)
+        work = torch.empty(kv4.hack_kv4_workspace(q, length, causal=causal, form=form), dtype=torch.uint8, device="cuda")
+        kv4.hack_kv4_attend(q, out, _ints(rows), length, workspace=work, causal=causal, form=form)
+        want = ref.attend(q[0].masked_fill(bad[..., None], 0), ref.values(planes.k_codes, planes.k_scales),
+                          ref.values(planes.v_codes, planes.v_scales), rows, tokens, dim ** -0.5, causal)
+        sees = torch.ones(tokens, dtype=torch.bool, device="cuda")
+        if causal:
+            sees = torch.arange(tokens, device="cuda") + rows - tokens >= 0
+        assert torch.isnan(out[0][bad & sees]).all()
+        assert (out[0][:, ~sees] == 0).all()
+        over = (out[0].double() - want[0]).abs() - ref.bound(*want, dtype, dim, rows)
+        assert over[~bad].max() <= 0
+    kv4.hack_kv4_poll_status()
+
+
+# ------------------------------------------------------------------ windows of few queries
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tokens,group", [(1, 1), (5, 2), (33, 1)])
+@pytest.mark.parametrize("window,n_sink", [(1, 0), (7, 4), (32, 0), (33, 40), (100, 3), (1000, 5)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_windows_of_few_queries(hb, dtype, tokens, group, window, n_sink, causal):
+    from tests.test_gpu_kv4 import _check
+    _check(hb, _gen(window), dtype, 128, 1, 3, group, tokens, 400, [400, 190, 12], causal=causal, window=window, n_sink=n_sink, form=1)
