@@ -177,3 +177,43 @@ def test_arrays_off_their_size_are_refused(hb):
                  lambda: bd.lib.hack_kv4_attend(k, a, 4096, 8192, 4096, 4098, None, None)):
         assert call() == 1 and "4 bytes" in hb.hack_last_error()
     assert bd.lib.hack_kv4_append(C.addressof(kv_off), r, 4096, 4096, 4096, None, None) == 1 and "8 bytes" in hb.hack_last_error()
+
+
+def test_marshalling_without_the_compiled_module(hb, monkeypatch):
+    """Where the module of csrc/pycall.c is not built, ctypes makes the same calls: the same keys, the same arguments in the same
+    places, the same answers."""
+    import os
+    import torch
+    from paper_2504_09261_b200 import binding as bd
+    exists = os.path.exists
+    monkeypatch.setattr(bd.os.path, "exists", lambda p: "_hackcall" not in str(p) and exists(p))
+    call, run = bd._load_call()
+    monkeypatch.undo()
+    assert run is not bd._run and bd._run.__class__.__name__ == "builtin_function_or_method"
+    assert call(bd._SCORE, 0, 0, 0, None, None, None, None) == bd._call(bd._SCORE, 0, 0, 0, None, None, None, None) == 1
+    x, ints = torch.zeros(2, 3, 4, 128), torch.zeros(4, dtype=torch.int32)
+    seen = []
+    # struct by struct as the entry points want them, with the sizes that each refuses by another text or serves without a launch
+    kv, plan = _kv4(), hb.hack_rope_plan(128)
+    strides = bd.HackStrides(1536, 512, 128)
+    for address, lead, tensors, structs in (
+            (bd._ROPE, plan, (x, x, ints), [bd.HackRopeArgs(0, 0, 2, 3, n, 0, 0, 0, 0, strides, bd.HackStrides(s, 512, 128)) for n, s in ((0, 1536), (4, 0), (-1, 0))]),
+            (bd._QK_NORM_ROPE, plan, (x, x, None, x, None, None, ints, None, None, None, None), [bd.HackQkvArgs(0, 0, 2, 3, 3, 4, 128, 1, 1e-6)]),
+            (bd._QK_NORM_ROPE, None, (x, None, None, x, None, None, ints, None, None, None, None), [bd.HackQkvArgs(0, 0, 2, 3, 3, 4, 128, 1, 1e-6)]),
+            (bd._KV4_APPEND, kv, (x, None, ints, None), [bd.HackKv4Rows(0, 4, strides, strides), bd.HackKv4Rows(0, 0)]),
+            (bd._KV4_APPEND, kv, (x, x, None, ints), [bd.HackKv4Rows(0, 4, strides, strides)]),
+            (bd._KV4_READ, kv, (x, x, None), [bd.HackKv4Rows(0, 4, strides, strides), bd.HackKv4Rows(0, 0)]),
+            (bd._KV4_ATTEND, kv, (x, x, None, None, None), [_attend(), _attend(n_queries=0)]),
+            (bd._KV4_ATTEND, kv, (x, None, ints, None, None), [_attend()])):
+        for args in structs:
+            store, lead_at = {}, None if lead is None else C.addressof(lead)
+            key = run(store, "head", address, lead_at, None, *tensors)
+            assert key == bd._run(store, "head", address, lead_at, None, *tensors) and key.__class__ is tuple and not store
+            store[key] = (args, C.addressof(args))
+            answers = []
+            for f in (run, bd._run):
+                status = f(store, "head", address, lead_at, None, *tensors)
+                answers.append((status, hb.hack_last_error() if status else ""))
+            assert answers[0] == answers[1] and answers[0][0].__class__ is int, answers
+            seen.append(answers[0])
+    assert {s for s, _ in seen} == {0, 1} and len({t for _, t in seen}) >= 6, seen
