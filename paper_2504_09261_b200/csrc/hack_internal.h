@@ -177,7 +177,8 @@ inline void launch_k(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem,
 // with its bound before it is used; on a violation the access is skipped and the code of the site
 // goes to the status word (nothing traps), which hack_poll_status reports.  The planes of a checked
 // build also carry a canary row behind every head, verified on the host by hack_debug_check.  In
-// the normal build the test is constant-true and costs nothing.
+// the normal build the test is constant-true and costs nothing.  (A 4-bit cache is the caller's, with
+// lengths and first rows in the caller's device arrays: its kernels hold them against the planes in every build.)
 constexpr int kDebugCodeBase = 100;     // status codes of the bounds checks start here
 constexpr unsigned char kCanaryByte = 0x5A;
 #if defined(__CUDACC__)

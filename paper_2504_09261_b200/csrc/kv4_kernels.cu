@@ -33,6 +33,8 @@ struct RowsParams {
   const int32_t* src_row;             // [heads] first row, or NULL
   const uint8_t* is_ctx;              // [kv_heads] type of a head
   int src_len[2];                     // rows of a head of each type
+  int src_cap[2];                     // and those it has room for (checked build)
+  int* status;
 };
 
 // 16 elements of a row as words; `whole`: they start on a 32-byte boundary.
@@ -174,7 +176,8 @@ __global__ void __launch_bounds__(kThreads) kv4_append_kernel(const __grid_const
   const int b = head / p.kv_heads, h = head - b * p.kv_heads;
   const T *k = static_cast<const T*>(p.k) + block * kBlock, *v = static_cast<const T*>(p.v) + block * kBlock;
   if (p.src_row) {
-    if (token >= p.src_len[p.is_ctx[h] ? 1 : 0]) return;
+    const int type = p.is_ctx[h] ? 1 : 0;
+    if (token >= p.src_len[type] || !dbg_ok(p.src_row[head] >= 0 && token < p.src_cap[type], p.status, 15)) return;
     const long long at = ((long long)p.src_row[head] + token) * (BLOCKS * kBlock);
     k += at;
     v += at;
@@ -336,9 +339,11 @@ hack_status_t launch_store_kv4(const StepArgs& a, int dtype, const hack_kv4_t* k
   p.lens = lens;
   p.src_row = a.row_off;
   p.is_ctx = a.is_ctx;
+  p.status = a.status;
   int longest = 0;
   for (int t = 0; t < 2; ++t) {
     p.src_len[t] = a.kept[t];
+    p.src_cap[t] = a.cap[t];
     if (a.heads_of[t] > 0 && a.kept[t] > longest) longest = a.kept[t];
   }
   p.n_tokens = longest;
