@@ -302,14 +302,14 @@ def _keep(key, args):
     _args_of[key] = (args, C.addressof(args))
 
 
-def _first(head, make, address, lead, stream, *tensors):
+def _first(head, args, address, lead, stream, *tensors):
     """A call that found no struct.  head holds plain numbers by now: a tensor of one element, say, would be held by its identity,
     and found again with another value in it."""
     while True:                       # (another thread may empty the store between the two lines below)
         status = _run(_args_of, head, address, lead, stream, *tensors)
         if status.__class__ is not tuple:
             return status
-        _keep(status, make())
+        _keep(status, args)
 
 
 def hack_rope_plan(head_dim: int, rotary_dim: Optional[int] = None, layout: int = HACK_ROPE_HALF, axes: int = 1,
@@ -328,7 +328,7 @@ def hack_rope(plan: HackRopePlan, x, y, positions, transpose: bool = False, stre
     status = _run(_args_of, head, _ROPE, C.addressof(plan), stream, x, y, positions)
     if status.__class__ is tuple:
         transpose = bool(transpose)
-        status = _first(("rope", plan.axes, plan.head_dim, transpose), lambda: _rope_args(plan, x, y, positions, transpose), _ROPE,
+        status = _first(("rope", plan.axes, plan.head_dim, transpose), _rope_args(plan, x, y, positions, transpose), _ROPE,
                         C.addressof(plan), stream, x, y, positions)
     if status:
         _check(status)
@@ -376,7 +376,7 @@ def hack_qk_norm_rope(plan: Optional[HackRopePlan], q, k, v, q_out, k_out, v_out
     if status.__class__ is tuple:
         norm, eps = operator.index(norm), float(eps)
         status = _first(("qkv", of_plan, norm, eps),
-                        lambda: _qkv_args(plan, q, k, v, q_out, k_out, v_out, positions, norm, eps, q_weight, k_weight, q_gain, k_gain),
+                        _qkv_args(plan, q, k, v, q_out, k_out, v_out, positions, norm, eps, q_weight, k_weight, q_gain, k_gain),
                         _QK_NORM_ROPE, lead, stream, q, k, v, q_out, k_out, v_out, positions, q_weight, k_weight, q_gain, k_gain)
     if status:
         _check(status)
@@ -424,14 +424,14 @@ class HackKv4:
     def hack_kv4_append(self, k, v, lens, new_lens=None, stream=None) -> None:
         status = _run(_args_of, self._head, _KV4_APPEND, self._address, stream, k, v, lens, new_lens)
         if status.__class__ is tuple:
-            status = _first(self._head, lambda: self._rows(k, v, lens, new_lens), _KV4_APPEND, self._address, stream, k, v, lens, new_lens)
+            status = _first(self._head, self._rows(k, v, lens, new_lens), _KV4_APPEND, self._address, stream, k, v, lens, new_lens)
         if status:
             _check(status)
 
     def hack_kv4_read(self, k_out, v_out, first, stream=None) -> None:
         status = _run(_args_of, self._head, _KV4_READ, self._address, stream, k_out, v_out, first)
         if status.__class__ is tuple:
-            status = _first(self._head, lambda: self._rows(k_out, v_out, first, None), _KV4_READ, self._address, stream, k_out, v_out, first)
+            status = _first(self._head, self._rows(k_out, v_out, first, None), _KV4_READ, self._address, stream, k_out, v_out, first)
         if status:
             _check(status)
 
@@ -467,7 +467,7 @@ class HackKv4:
             max_len, n_sink, window, form = map(operator.index, (max_len, n_sink, window, form))
             appended, causal, sm_scale = bool(appended), bool(causal), float(sm_scale)
             status = _first((self._head, max_len, appended, causal, n_sink, window, sm_scale, form),
-                            lambda: self._attend(q, out, lens, max_len, new_lens, appended, causal, n_sink, window, sm_scale, room, form),
+                            self._attend(q, out, lens, max_len, new_lens, appended, causal, n_sink, window, sm_scale, room, form),
                             _KV4_ATTEND, self._address, stream, q, out, lens, new_lens, workspace)
         if status:
             _check(status)
