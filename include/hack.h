@@ -434,14 +434,17 @@ enum { HACK_KV4_FEW = 1,         /* 8 or 16 query rows a CTA, any type */
        HACK_KV4_MANY = 2 };      /* tiles of 128 query rows, bf16 */
 /* Device memory that a call of these sizes needs (it may be 0); it depends on the struct's sizes alone. */
 HACK_API hack_status_t hack_kv4_workspace(const hack_kv4_t* kv, const hack_kv4_attend_t* args, size_t* bytes);
-/* O = Softmax(sm_scale Q K^T) V over the stored rows that a query sees; a query that sees none gets zeros.  Logits,
- * softmax and sums in fp32.  workspace: 16-byte aligned, its contents need no preparation and mean nothing after the call;
+/* O = Softmax(sm_scale Q K^T) V over the stored rows that a query sees; a query that sees none gets zeros, one with a NaN
+ * that sees any NaN.  Logits, softmax and sums are fp32 numbers; in bf16 calls a probability p is rounded to bf16 once, for the
+ * product with the values and for the sum it is divided by alike, which moves a result by at most 2^-8 sum p |v - out| besides
+ * its own rounding (2^-8 |out|).  workspace: 16-byte aligned, its contents need no preparation and mean nothing after the call;
  * calls that may overlap on the GPU need workspaces of their own. */
 HACK_API hack_status_t hack_kv4_attend(const hack_kv4_t* kv, const hack_kv4_attend_t* args, const void* q, void* out,
                                        const int32_t* lens, const int32_t* new_lens, void* workspace, void* stream);
 
 /* Synchronises `stream`, then reports whether a bounded device-side wait of hack_kv4_attend on this device gave up since the
- * last call: HACK_OK or HACK_ERR_TIMEOUT (what that call wrote is undefined). */
+ * last call: HACK_OK or HACK_ERR_TIMEOUT (what that call wrote is undefined).  Nothing else reports it: hack_poll_status is about
+ * a cache's own steps.  A loop of calls asks once where it reads its results. */
 HACK_API hack_status_t hack_kv4_poll_status(int32_t device, void* stream);
 
 /* Text of the calling thread's last error; never NULL. */

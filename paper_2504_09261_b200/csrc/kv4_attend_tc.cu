@@ -15,6 +15,8 @@
 // next Q K^T runs under it; the output is rescaled only when a row's maximum grows by more than 2^32.
 // A CTA that is through with a unit takes over one that has not been launched yet (cluster launch control): its queries and
 // first tiles are on their way under the last softmax and the output of the unit before.
+// A probability is rounded to bf16 once, for the product with the values and the row's sum alike: the product takes bf16, and a
+// second one for the rest would be half as much work again for the tensor pipe, one of the three resources that bound it.
 // Every wait is bounded; a CTA that gives up lets its products end, frees its tensor memory and raises the status word.
 #include <algorithm>
 #include <type_traits>
