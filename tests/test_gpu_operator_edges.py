@@ -169,3 +169,64 @@ def test_queries_with_no_numbers_and_infinities(hb, dtype, form, dim, tokens, le
 def test_windows_of_few_queries(hb, dtype, tokens, group, window, n_sink, causal):
     from tests.test_gpu_kv4 import _check
     _check(hb, _gen(window), dtype, 128, 1, 3, group, tokens, 400, [400, 190, 12], causal=causal, window=window, n_sink=n_sink, form=1)
+
+
+# ------------------------------------------------------------------ calls that the header allows
+@pytest.mark.parametrize("dtype,form,tokens,cap", [(torch.float32, 1, 1, 60000), (torch.float32, 1, 40, 3000), (torch.bfloat16, 1, 1, 60000), (torch.bfloat16, 1, 7, 2000),
+                                                   (torch.bfloat16, 2, 300, 200), (torch.bfloat16, 2, 130, 9000)])
+def test_attention_in_place(hb, dtype, form, tokens, cap):
+    """The output is the queries' own tensor, with one CTA to a tile, a cluster, and partial results."""
+    from tests.test_gpu_kv4 import Planes
+    g, heads, dim = _gen(tokens), 2, 64
+    planes = Planes(heads * cap, dim)
+    planes.randomise(g)
+    kv4 = planes.handle(hb, 1, heads, cap)
+    q = torch.randn(1, heads * 3, tokens, dim, generator=g, device="cuda").to(dtype)
+    out, lens = torch.empty_like(q), _ints(cap, cap // 2)
+    work = torch.empty(kv4.hack_kv4_workspace(q, cap, form=form), dtype=torch.uint8, device="cuda")
+    kv4.hack_kv4_attend(q, out, lens, cap, workspace=work, form=form)
+    kv4.hack_kv4_attend(q, q, lens, cap, workspace=work, form=form)
+    assert torch.equal(q, out)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_norm_and_rotation_in_place(hb, dtype):
+    """All three parts where they lie in the projection's output."""
+    g = _gen(17)
+    qkv = torch.randn(2, 19, 8 + 2 * 2, 128, generator=g, device="cuda").to(dtype)
+    parts = lambda x: [x[:, :, a:b].transpose(1, 2) for a, b in ((0, 8), (8, 10), (10, 12))]   # noqa: E731
+    plan, pos = hb.hack_rope_plan(128, 96), torch.arange(19, dtype=torch.int32, device="cuda")
+    outs = [torch.empty(x.shape, dtype=dtype, device="cuda") for x in parts(qkv)]
+    hb.hack_qk_norm_rope(plan, *parts(qkv), *outs, pos)
+    before = qkv.clone()
+    hb.hack_qk_norm_rope(plan, *parts(qkv), *parts(qkv), pos)
+    assert all(torch.equal(x, y) for x, y in zip(parts(qkv), outs))
+    assert torch.equal(qkv[:, :, 10:], before[:, :, 10:])
+
+
+def test_threads_on_streams_of_their_own(hb):
+    """Calls of several threads at once, each of sizes that the binding has not seen and of sizes that it has."""
+    import threading
+    plan, wrong = hb.hack_rope_plan(64), []
+    f = rope_ref.frequencies(64, 1)
+
+    def work(i):
+        try:
+            stream, g = torch.cuda.Stream(), _gen(i)
+            with torch.cuda.stream(stream):
+                for r in range(60):
+                    n = 1 + (7 * r + i) % 25
+                    x = torch.randn(1, 3, n, 64, generator=g, device="cuda")
+                    y, pos = torch.empty_like(x), torch.arange(n, dtype=torch.int32, device="cuda")
+                    hb.hack_rope(plan, x, y, pos, stream=stream.cuda_stream)
+                    want, size = rope_ref.rotate(x, pos, 64, 0, 1, *f)
+                    assert ((y.double() - want).abs() <= rope_ref.bound(want, size, x.dtype)).all()
+        except Exception as e:                               # noqa: BLE001  (told to the test's own thread)
+            wrong.append(repr(e))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong, wrong
